@@ -698,6 +698,103 @@ int calibatt_merge_intervals(const uint8_t *mask, int64_t n_rows, int nbk, doubl
 int calibatt_share_timesteps(const uint8_t *masks, int T, int64_t n, double tau, int32_t *cluster,
                              uint8_t *shared, int32_t *n_clusters);
 
+/* ---- Around the attention: positions, normalisation --------------------- */
+
+/* Element types of these calls: CALIBATT_BF16, CALIBATT_F16 and */
+enum { CALIBATT_F32 = 2 };
+
+/*
+ * Rotary positions with several axes (time, height, width of a video's tokens).
+ * Axis a has dims[a] / 2 pairs of channels; pair i of it turns by the angle
+ *   pos_a * scale[a] * theta^(-2 i / dims[a])
+ *   (x, y) -> (x cos - y sin, x sin + y cos).
+ * The axes' pairs follow each other: pair j of all P = sum(dims) / 2 is made of
+ * channels 2j and 2j + 1 (interleaved) or j and j + P.  Channels from 2P on are
+ * copied.
+ *
+ * calibatt_rope_table (host): the cosines and sines of positions 0 .. length[a]-1
+ * of every axis, computed in 64 bits and rounded to fp32, as
+ * [axis][position][pair][cos, sin].  *entries receives their number (pairs of
+ * floats); table NULL = only that.  scale NULL = all ones.
+ * Errors: NULL; UNSUPPORTED (n_axes outside 1..4); SHAPE (an odd or negative
+ * dims[a], none or more than 1024 channels in all, length[a] <= 0, theta not
+ * positive and finite, scale not finite, more than 2^30 - 1 entries);
+ * BUFFER_TOO_SMALL (capacity, in entries).
+ */
+int calibatt_rope_table(int n_axes, const int32_t *dims, const int32_t *length, const double *scale,
+                        double theta, float *table, int64_t capacity, int64_t *entries);
+
+typedef struct calibatt_rope {
+  int32_t n_axes, interleaved;
+  int32_t dims[4], length[4];
+  const float *table; /* DEVICE, as calibatt_rope_table fills it */
+} calibatt_rope;
+
+/* Where the tokens are.  positions NULL: the first grid[0] * .. tokens are a
+ * row-major grid whose first token is at start[]; tokens behind it are copied.
+ * Else DEVICE int32, token n of batch entry b at [b * positions_b + n * n_axes]
+ * (positions_b 0: the same for all); a negative position leaves its axis's
+ * pairs as they are, one that the table does not reach turns them into NaN. */
+typedef struct calibatt_rope_place {
+  int32_t grid[4], start[4];
+  const int32_t *positions;
+  int64_t positions_b;
+} calibatt_rope_place;
+
+/*
+ * Turns q [B][Hq][N][D] and, unless NULL, k [B][Hk][N][D] in one launch.  With
+ * `inverse` the angles are negated: that is the way back, and the gradient with
+ * respect to the input for a given gradient of the output.  Strides as in
+ * calibatt_sparse_attn_fwd_strided (NULL = packed; every one a multiple of 8, n
+ * >= D, pointers 16-byte aligned; no limit on a head's bytes).  An output may be
+ * its own input with the same strides and must not overlap an input otherwise.
+ * Arithmetic is fp32, rounded once.
+ * Errors: NULL; SHAPE (also: more channels than D, a grid of more than N tokens
+ * or beyond the tables, B or a number of heads above 65535); UNSUPPORTED (dtype,
+ * D not a multiple of 8 or above 1024, P not a multiple of 4, or of 8 where not
+ * interleaved); LAUNCH.
+ */
+int calibatt_rope_axes(const void *q, void *q_out, const void *k, void *k_out, int B, int Hq, int Hk,
+                       int N, int D, const calibatt_rope *rope, const calibatt_rope_place *place,
+                       const calibatt_strides *q_strides, const calibatt_strides *q_out_strides,
+                       const calibatt_strides *k_strides, const calibatt_strides *k_out_strides,
+                       int dtype, int inverse, void *stream);
+
+/*
+ * Layer norm over the last axis of x [B][H][N][C]:
+ *   y = (x - mean) / sqrt(mean((x - mean)^2) + eps) * weight + bias,
+ * with mean = 0 unless `center` (root mean square).  weight [C] NULL = ones, bias
+ * [C] NULL = zeros (a bias needs a weight); both of weight_dtype, which is dtype
+ * or CALIBATT_F32.  Any strides >= 0 of b, h, n (NULL = packed); C contiguous.
+ * Rows of whole, aligned 16-byte pieces take 16-byte accesses, others go element
+ * by element.  y may be x with the same strides.  Statistics and arithmetic are
+ * fp32, rounded once.
+ * Errors: NULL (also a bias without a weight); SHAPE (non-positive sizes, more
+ * than 2^30 - 1 rows, eps negative or not a number, misaligned elements);
+ * UNSUPPORTED (types, C above 8192); LAUNCH.
+ */
+int calibatt_layer_norm_fwd(const void *x, const void *weight, const void *bias, void *y, int64_t B,
+                            int64_t H, int64_t N, int C, const calibatt_strides *x_strides,
+                            const calibatt_strides *y_strides, float eps, int center, int dtype,
+                            int weight_dtype, void *stream);
+
+/*
+ * Its gradients for dy, the gradient of y: dx [B][H][N][C], and dweight, dbias [C]
+ * of weight_dtype where they are not NULL.  Nothing of the forward is needed but x.
+ * The rows' contributions to dweight and dbias are added up in an order that
+ * depends on the sizes and the device alone.  workspace: DEVICE, at least
+ * calibatt_layer_norm_bwd_workspace_bytes(C) of the current device; only where
+ * dweight or dbias is asked for.  dx may be dy or x with the same strides.
+ * Errors: as calibatt_layer_norm_fwd; NULL (dweight or dbias without weight or
+ * workspace); BUFFER_TOO_SMALL.
+ */
+int calibatt_layer_norm_bwd_workspace_bytes(int C, int64_t *bytes);
+int calibatt_layer_norm_bwd(const void *dy, const void *x, const void *weight, void *dx, void *dweight,
+                            void *dbias, int64_t B, int64_t H, int64_t N, int C,
+                            const calibatt_strides *dy_strides, const calibatt_strides *x_strides,
+                            const calibatt_strides *dx_strides, float eps, int center, int dtype,
+                            int weight_dtype, float *workspace, int64_t workspace_bytes, void *stream);
+
 /* Static, NUL-terminated description of a status code. */
 const char *calibatt_strerror(int status);
 

@@ -186,6 +186,9 @@ def load_library():
     lib.calibatt_strerror.argtypes = [C.c_int]
     lib.calibatt_version.restype = C.c_int
     lib.calibatt_version.argtypes = []
+    from . import layer_ops
+
+    layer_ops.declare(lib)
     _lib = lib
     return lib
 

@@ -1,0 +1,279 @@
+"""ctypes marshalling of what a layer does around its attention: rotary positions with several axes, layer norm
+and its gradients.  As in ``binding``: every step runs in the C/HIP library, torch supplies buffers and streams."""
+from __future__ import annotations
+
+import contextlib
+import ctypes as C
+from typing import Optional, Sequence
+
+import numpy as np
+
+from . import binding as _b
+
+_NO_SWITCH = contextlib.nullcontext()
+
+
+class _CRope(C.Structure):
+    _fields_ = [("n_axes", C.c_int32), ("interleaved", C.c_int32), ("dims", C.c_int32 * 4), ("length", C.c_int32 * 4),
+                ("table", C.c_void_p)]
+
+
+class _CRopePlace(C.Structure):
+    _fields_ = [("grid", C.c_int32 * 4), ("start", C.c_int32 * 4), ("positions", C.c_void_p), ("positions_b", C.c_int64)]
+
+
+def declare(lib):
+    """Argument types of the calls of this module."""
+    i32p, f32p, i64p = C.POINTER(C.c_int32), C.POINTER(C.c_float), C.POINTER(C.c_int64)
+    lib.calibatt_rope_table.restype = C.c_int
+    lib.calibatt_rope_table.argtypes = [C.c_int, i32p, i32p, C.POINTER(C.c_double), C.c_double, f32p, C.c_int64, i64p]
+    lib.calibatt_rope_axes.restype = C.c_int
+    lib.calibatt_rope_axes.argtypes = [C.c_void_p] * 4 + [C.c_int] * 5 + [C.c_void_p] * 6 + [C.c_int, C.c_int, C.c_void_p]
+    lib.calibatt_layer_norm_fwd.restype = C.c_int
+    lib.calibatt_layer_norm_fwd.argtypes = [C.c_void_p] * 4 + [C.c_int64] * 3 + [C.c_int] + [C.c_void_p] * 2 + [
+        C.c_float, C.c_int, C.c_int, C.c_int, C.c_void_p]
+    lib.calibatt_layer_norm_bwd_workspace_bytes.restype = C.c_int
+    lib.calibatt_layer_norm_bwd_workspace_bytes.argtypes = [C.c_int, i64p]
+    lib.calibatt_layer_norm_bwd.restype = C.c_int
+    lib.calibatt_layer_norm_bwd.argtypes = [C.c_void_p] * 6 + [C.c_int64] * 3 + [C.c_int] + [C.c_void_p] * 3 + [
+        C.c_float, C.c_int, C.c_int, C.c_int, C.c_void_p, C.c_int64, C.c_void_p]
+
+
+_dtypes = None
+
+
+def _dtype_of(t):
+    """The library's number of a tensor's element type, or None."""
+    global _dtypes
+    if _dtypes is None:
+        import torch
+
+        _dtypes = {torch.bfloat16: 0, torch.float16: 1, torch.float32: 2}
+    return _dtypes.get(t.dtype)
+
+
+def _on(device):
+    """Context in which ``device`` is the current one: kernels are launched on the current device."""
+    import torch
+
+    return _NO_SWITCH if device.index == torch.cuda.current_device() else torch.cuda.device(device)
+
+
+def _empty_like(t, other):
+    """``torch.empty_like`` of the call's stream (see ``binding._stream_of``), to be returned."""
+    import torch
+
+    if other is None:
+        return torch.empty_like(t)
+    current = torch.cuda.current_stream(t.device)
+    with torch.cuda.stream(other):
+        out = torch.empty_like(t)
+    out.record_stream(current)
+    return out
+
+
+def _strides(*tensors):
+    """The b, h, n strides of [B, H, N, D] tensors as one array of int64, and the address of each tensor's three."""
+    flat = []
+    for t in tensors:
+        flat += t.stride()[:3]
+    array = (C.c_int64 * len(flat))(*flat)
+    at = C.addressof(array)
+    return array, [at + 24 * i for i in range(len(tensors))]
+
+
+class RotaryAxes:
+    """Cosines and sines of rotary positions with several axes, on the GPU.
+
+    ``dims``: channels of each axis (even; their pairs follow each other), ``lengths``: positions that each axis may
+    take, ``scale``: factor of each axis's positions.  ``interleaved``: pairs are channels 2j and 2j + 1, else j and j +
+    sum(dims) / 2.  Pair i of an axis turns by pos * scale * theta^(-2 i / dims).  The angles are computed in 64 bits."""
+
+    def __init__(self, dims: Sequence[int], lengths: Sequence[int], theta: float = 10000.0,
+                 scale: Optional[Sequence[float]] = None, interleaved: bool = True, device="cuda"):
+        import torch
+
+        lib = _b.load_library()
+        self.dims, self.lengths = tuple(int(d) for d in dims), tuple(int(n) for n in lengths)
+        if not (1 <= len(self.dims) <= 4 and len(self.lengths) == len(self.dims)):
+            raise ValueError("one to four axes, with as many lengths")
+        if scale is not None and len(scale) != len(self.dims):
+            raise ValueError("one scale per axis")
+        n = len(self.dims)
+        d, ln = (C.c_int32 * n)(*self.dims), (C.c_int32 * n)(*self.lengths)
+        sc = None if scale is None else (C.c_double * n)(*(float(s) for s in scale))
+        entries = C.c_int64(0)
+        st = lib.calibatt_rope_table(n, d, ln, sc, float(theta), None, 0, C.byref(entries))
+        if st == 0:
+            host = np.empty((max(entries.value, 1), 2), np.float32)
+            st = lib.calibatt_rope_table(n, d, ln, sc, float(theta), _b._ptr(host, C.c_float), entries.value, C.byref(entries))
+        if st != 0:
+            raise _b.CalibattError(st, "calibatt_rope_table")
+        self.interleaved = bool(interleaved)
+        self.host_table = host
+        self.table = torch.from_numpy(host).to(device)
+        self._c = _CRope(n, 1 if interleaved else 0, (C.c_int32 * 4)(*self.dims), (C.c_int32 * 4)(*self.lengths),
+                         self.table.data_ptr())
+        self._c_at = C.addressof(self._c)
+        self._grids = {}  # (grid, start) -> struct
+
+    def _place(self, grid, start, positions):
+        if positions is not None:
+            return _CRopePlace((C.c_int32 * 4)(), (C.c_int32 * 4)(), positions.data_ptr(),
+                               positions.stride(0) if positions.dim() == 3 else 0)
+        key = (tuple(grid), tuple(start))
+        place = self._grids.get(key)
+        if place is None:
+            n = len(self.dims)
+            if len(key[0]) != n or len(key[1]) != n:
+                raise ValueError(f"grid and start have one entry per axis ({n})")
+            if len(self._grids) >= 64:  # a stream's start moves on: old places are of no use
+                self._grids.clear()
+            place = self._grids[key] = _CRopePlace((C.c_int32 * 4)(*key[0]), (C.c_int32 * 4)(*key[1]), None, 0)
+        return place
+
+
+def rope_axes(q, k, rope: RotaryAxes, grid=None, start=None, positions=None, q_out=None, k_out=None, inverse: bool = False,
+              stream=None):
+    """calibatt_rope_axes on CUDA tensors q [B, Hq, N, D] and k [B, Hk, N, D] (or None) of one element type (bf16, fp16 or
+    fp32), strided views with contiguous D allowed; returns (q_out, k_out), new tensors unless given.
+
+    ``grid``: the first grid[0] * grid[1] * ... tokens are that row-major grid, the first of them at ``start`` (default: all
+    zeros); tokens behind it are copied.  Or ``positions``: int32 CUDA tensor [N, axes] or [B, N, axes]; a negative position
+    leaves the axis's channels as they are, one behind the table's length gives NaN.  ``inverse`` turns back: with it the
+    call takes a gradient of its outputs to that of its inputs.  ``q_out=q, k_out=k`` turns in place."""
+    lib = _b.load_library()
+    shape, dtype = q.shape, _dtype_of(q)
+    if not (q.is_cuda and dtype is not None and len(shape) == 4 and q.stride(3) == 1):
+        raise ValueError("q must be a bf16, fp16 or fp32 CUDA tensor [B, H, N, D] with contiguous D")
+    if k is not None and not (k.dtype == q.dtype and k.device == q.device and k.dim() == 4 and k.stride(3) == 1
+                              and k.shape[0] == shape[0] and k.shape[2:] == shape[2:]):
+        raise ValueError("k must have q's element type, device and shape but for the heads, with contiguous D")
+    if (grid is None) == (positions is None):
+        raise ValueError("either a grid or positions")
+    if positions is None:
+        start = (0,) * len(rope.dims) if start is None else start
+    else:
+        import torch
+
+        n = len(rope.dims)
+        if start is not None:
+            raise ValueError("start belongs to a grid")
+        if not (positions.device == q.device and positions.dtype == torch.int32
+                and tuple(positions.shape) in ((shape[2], n), (shape[0], shape[2], n))
+                and positions.stride(-1) == 1 and positions.stride(-2) == n):
+            raise ValueError(f"positions must be an int32 CUDA tensor [N, {n}] or [B, N, {n}] with contiguous rows")
+    if rope.table.device != q.device:
+        raise ValueError("the tables of the axes are on another device")
+    stream, other = _b._stream_of(stream, q.device)
+    for x, x_out in ((q, q_out), (k, k_out)):
+        if x_out is not None and (x is None or not (x_out.shape == x.shape and x_out.dtype == x.dtype and x_out.device == x.device
+                                                    and x_out.stride(3) == 1)):
+            raise ValueError("an output must have its input's shape, element type and device, with contiguous D")
+    with _on(q.device):
+        if q_out is None:
+            q_out = _empty_like(q, other)
+        if k is not None and k_out is None:
+            k_out = _empty_like(k, other)
+        place = rope._place(grid, start, positions)
+        if k is None:
+            keep, at = _strides(q, q_out)
+            at += [None, None]
+            hk, kp, kop = 0, None, None
+        else:
+            keep, at = _strides(q, q_out, k, k_out)
+            hk, kp, kop = k.shape[1], k.data_ptr(), k_out.data_ptr()
+        st = lib.calibatt_rope_axes(q.data_ptr(), q_out.data_ptr(), kp, kop, shape[0], shape[1], hk, shape[2], shape[3],
+                                    rope._c_at, C.addressof(place), *at, dtype, 1 if inverse else 0, stream)
+    if st != 0:
+        raise _b.CalibattError(st, "calibatt_rope_axes")
+    return q_out, k_out
+
+
+def _rows(t, what):
+    """(shape, strides) of a tensor [..., C] as three indices of rows."""
+    if not (t.is_cuda and 1 <= t.dim() <= 4 and _dtype_of(t) is not None and (t.stride(-1) == 1 or t.shape[-1] == 1)):
+        raise ValueError(f"{what} must be a bf16, fp16 or fp32 CUDA tensor of one to four axes with a contiguous last one")
+    pad = 4 - t.dim()
+    return (1,) * pad + tuple(t.shape[:-1]), (0,) * pad + t.stride()[:-1]
+
+
+def _norm_arguments(x, weight, bias, others):
+    """Checks, and (n0, n1, n2, C, strides of x and of every tensor of ``others``, their array)."""
+    rows, s = _rows(x, "x")
+    flat = list(s)
+    for name, t in others:
+        if not (t.shape == x.shape and t.dtype == x.dtype and t.device == x.device):
+            raise ValueError(f"{name} must have the shape, element type and device of x")
+        flat += _rows(t, name)[1]
+    if bias is not None and weight is None:
+        raise ValueError("a bias needs a weight")
+    for t in (weight, bias):
+        if t is not None and not (t.device == x.device and tuple(t.shape) == tuple(x.shape[-1:]) and t.is_contiguous()
+                                  and _dtype_of(t) in (_dtype_of(x), 2) and t.dtype == weight.dtype):
+            raise ValueError("weight and bias must be contiguous [C] on x's device, both of x's element type or both fp32")
+    array = (C.c_int64 * len(flat))(*flat)
+    return rows, array, C.addressof(array)
+
+
+def layer_norm_fwd(x, weight=None, bias=None, eps: float = 1e-6, center: bool = True, out=None, stream=None):
+    """calibatt_layer_norm_fwd over the last axis of a CUDA tensor [..., C] of one to four axes (bf16, fp16 or fp32; views
+    with a contiguous last axis).  ``weight``, ``bias``: [C] of x's element type or fp32, or None.  ``center=False``: root
+    mean square, no mean is taken off.  Returns a new tensor, or ``out`` (which may be x)."""
+    lib = _b.load_library()
+    if not x.is_cuda:
+        raise ValueError("x must be a CUDA tensor")
+    stream, other = _b._stream_of(stream, x.device)
+    with _on(x.device):
+        y = _empty_like(x, other) if out is None else out
+        rows, keep, at = _norm_arguments(x, weight, bias, (("out", y),))
+        dtype = _dtype_of(x)
+        st = lib.calibatt_layer_norm_fwd(x.data_ptr(), None if weight is None else weight.data_ptr(),
+                                         None if bias is None else bias.data_ptr(), y.data_ptr(), *rows, x.shape[-1], at,
+                                         at + 24, float(eps), 1 if center else 0, dtype,
+                                         dtype if weight is None else _dtype_of(weight), stream)
+    if st != 0:
+        raise _b.CalibattError(st, "calibatt_layer_norm_fwd")
+    return y
+
+
+_norm_workspace_rows = {}  # device index -> bytes of the workspace for one column
+
+
+def layer_norm_bwd(dy, x, weight=None, bias=None, eps: float = 1e-6, center: bool = True, dx=None, stream=None):
+    """calibatt_layer_norm_bwd: (dx, dweight, dbias) for ``dy``, the gradient of what ``layer_norm_fwd`` gives for the same
+    x, weight and bias (of the bias only its presence counts).  dweight and dbias have their parameter's type, None where
+    there is none.  ``dx``: optional tensor to receive the gradient of x, which may be dy or x."""
+    import torch
+
+    lib = _b.load_library()
+    if not x.is_cuda:
+        raise ValueError("x must be a CUDA tensor")
+    stream, other = _b._stream_of(stream, x.device)
+    with _on(x.device):
+        to = _empty_like(x, other) if dx is None else dx
+        rows, keep, at = _norm_arguments(x, weight, bias, (("dy", dy), ("dx", to)))
+        width, dtype = x.shape[-1], _dtype_of(x)
+        dweight = dbias = workspace = None
+        nbytes = 0
+        if weight is not None:
+            per_column = _norm_workspace_rows.get(x.device.index)
+            if per_column is None:
+                n = C.c_int64(0)
+                st = lib.calibatt_layer_norm_bwd_workspace_bytes(1, C.byref(n))
+                if st != 0:
+                    raise _b.CalibattError(st, "calibatt_layer_norm_bwd_workspace_bytes")
+                per_column = _norm_workspace_rows[x.device.index] = n.value
+            nbytes = per_column * width
+            workspace = _b._empty(nbytes // 4, torch.float32, x.device, other)
+            dweight = _empty_like(weight, other)
+            dbias = None if bias is None else _empty_like(bias, other)
+        st = lib.calibatt_layer_norm_bwd(dy.data_ptr(), x.data_ptr(), None if weight is None else weight.data_ptr(),
+                                         to.data_ptr(), None if dweight is None else dweight.data_ptr(),
+                                         None if dbias is None else dbias.data_ptr(), *rows, width, at + 24, at, at + 48,
+                                         float(eps), 1 if center else 0, dtype,
+                                         dtype if weight is None else _dtype_of(weight),
+                                         None if workspace is None else workspace.data_ptr(), nbytes, stream)
+    if st != 0:
+        raise _b.CalibattError(st, "calibatt_layer_norm_bwd")
+    return to, dweight, dbias
