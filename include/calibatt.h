@@ -795,6 +795,51 @@ int calibatt_layer_norm_bwd(const void *dy, const void *x, const void *weight, v
                             const calibatt_strides *dx_strides, float eps, int center, int dtype,
                             int weight_dtype, float *workspace, int64_t workspace_bytes, void *stream);
 
+/*
+ * Attention in a window, with a few first keys that stay visible.
+ * The query at position p is in frame f = floor(p / frame) and sees the keys
+ * (key j is at position j) of frames f - left .. f + right, and of the first
+ * `sinks` keys those that are not behind frame f + right.  left, right -1: no
+ * limit.  frame 1: a window of tokens; frame = tokens per video frame: a window
+ * of whole frames.  right 0 with frame 1 is causal.
+ * Query i of batch entry b is at position i + offset, or, with q_start, at
+ * i + q_start[b].  k_len[b] (NULL: Nk): keys of entry b, the rows behind them
+ * hold anything; q_len[b] (NULL: Nq): its queries; rows behind them see nothing.
+ * All three are DEVICE int32 [B]; lengths are taken as between 0 and Nk or Nq,
+ * positions as within 2^30 of zero.
+ */
+typedef struct calibatt_window {
+  int32_t left, right, sinks, frame, offset;
+  const int32_t *q_start, *q_len, *k_len;
+} calibatt_window;
+
+/*
+ * calibatt_window_attn_fwd: q [B][Hq][Nq][D], k, v [B][Hkv][Nk][D], out like q,
+ * all bf16 or all fp16; Hq a multiple of Hkv, query head h reads key head
+ * h / (Hq / Hkv).  out = softmax(scale q K^T) V over the visible keys, fp32
+ * accumulation, probabilities rounded to the element type for the product with
+ * V; a query that sees no key gets zeros.  lse (NULL, or DEVICE fp32 packed
+ * [B][Hq][Nq]): the natural logarithm of the sum of exponentials, -inf there.
+ * Keys and values that no query of a call's block sees are not read; those that
+ * some query sees must be finite.
+ * workspace: DEVICE, calibatt_window_attn_workspace_bytes (0 where none is
+ * needed): calls of few queries are cut along the keys and joined.  NULL: they
+ * are not.  Calls that overlap on the GPU need workspaces of their own.
+ * Strides as in calibatt_sparse_attn_fwd_strided (NULL = packed; k and v share
+ * theirs); pointers 16-byte aligned.  Supported: D in {64, 128}.
+ * Errors: NULL; SHAPE (sizes not positive, Hq no multiple of Hkv, more than
+ * 2^31 - 1 rows, a window with left or right below -1, sinks < 0, frame <= 0 or
+ * |offset| > 2^30, strides, alignment, out an input, scale not finite);
+ * UNSUPPORTED (D, dtype); BUFFER_TOO_SMALL; LAUNCH.
+ */
+int calibatt_window_attn_workspace_bytes(int B, int Hq, int Hkv, int Nq, int Nk, int D,
+                                         const calibatt_window *window, int64_t *forward);
+int calibatt_window_attn_fwd(const void *q, const void *k, const void *v, void *out, float *lse, int B,
+                             int Hq, int Hkv, int Nq, int Nk, int D, const calibatt_window *window,
+                             float scale, const calibatt_strides *q_strides,
+                             const calibatt_strides *kv_strides, const calibatt_strides *out_strides,
+                             int dtype, void *workspace, int64_t workspace_bytes, void *stream);
+
 /* Static, NUL-terminated description of a status code. */
 const char *calibatt_strerror(int status);
 

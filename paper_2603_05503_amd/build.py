@@ -11,7 +11,7 @@ CSRC = os.path.join(PKG_DIR, "csrc")
 LIB_PATH = os.path.join(PKG_DIR, "libcalibatt.so")
 PROBE_PATH = os.path.join(PKG_DIR, "mfma_peak_probe.bin")  # stand-alone executable, see csrc/mfma_peak_probe.hip
 
-SOURCES = ["compile_pattern.cpp", "anchor_map.cpp", "calibration.cpp", "skiplist.cpp", "split_plan.cpp", "sparse_attn_fwd.hip", "sparse_attn_split.hip", "row_ops.hip"]
+SOURCES = ["compile_pattern.cpp", "anchor_map.cpp", "calibration.cpp", "skiplist.cpp", "split_plan.cpp", "sparse_attn_fwd.hip", "sparse_attn_split.hip", "row_ops.hip", "window_attn.hip"]
 
 # Packed fp32 VALU forms are switched off for all device code.
 HIP_FLAGS = [

@@ -74,8 +74,10 @@ constexpr __host__ __device__ int il_sub(int d, int bq, int bk) { return bk % 64
 // (20 heads of 32 760 tokens, key blocks of 64).
 constexpr __host__ __device__ int il_iv_cols(int bq) { return bq == 64 ? 1024 : IV_COLS; }
 
-// The base class lays out LDS and lanes for a window of two sub-tiles of K and of V.
-template <int D, int BQ, int BK, typename T = Bf16>
+// The base class lays out LDS and lanes for a window of two sub-tiles of K and of V.  EXACT_SUM: a row's sum is that of the
+// probabilities in fp32 and not of what they are rounded to for the second contraction (one more instruction per pair): a
+// log-sum-exp then has the precision that a gradient computed from it needs.
+template <int D, int BQ, int BK, typename T = Bf16, bool EXACT_SUM = false>
 struct IlRow : RowBlock<D, BQ, 2 * il_sub(D, BQ, BK), T> {
   using RB = RowBlock<D, BQ, 2 * il_sub(D, BQ, BK), T>;
   using RB::DB;
@@ -206,7 +208,13 @@ struct IlRow : RowBlock<D, BQ, 2 * il_sub(D, BQ, BK), T> {
       } else {
         // pairs 4 (g % 2) + [0,4) of sub-block g / 2 land on logits consumed above (this group or the one before)
         constexpr int i = o - 16;
-        named_pack_and_sum<T, B + 16 * (g / 2) + 4 * (g % 2) + i>(x[2 * i], x[2 * i + 1], psum[i & 1]);
+        if constexpr (EXACT_SUM) {
+          ordered_add(psum[0], x[2 * i]);
+          ordered_add(psum[1], x[2 * i + 1]);
+          named_pack<T, B + 16 * (g / 2) + 4 * (g % 2) + i>(x[2 * i], x[2 * i + 1]);
+        } else {
+          named_pack_and_sum<T, B + 16 * (g / 2) + 4 * (g % 2) + i>(x[2 * i], x[2 * i + 1], psum[i & 1]);
+        }
       }
     }
   }

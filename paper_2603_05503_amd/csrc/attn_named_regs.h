@@ -122,6 +122,17 @@ template <int R>
 __device__ __forceinline__ void named_write(uint32_t x) {
   asm volatile("v_mov_b32 v[%1], %0" : : "v"(x), "n"(R));
 }
+__device__ __forceinline__ void ordered_add(float &acc, float x) {
+  asm volatile("v_add_f32 %0, %0, %1" : "+v"(acc) : "v"(x));
+}
+// v[R] = (lo, hi) rounded to nearest-even and packed
+template <typename T, int R>
+__device__ __forceinline__ void named_pack(float lo, float hi) {
+  if constexpr (std::is_same<T, Bf16>::value)
+    asm volatile("v_cvt_pk_bf16_f32 v[%2], %0, %1" : : "v"(lo), "v"(hi), "n"(R));
+  else
+    asm volatile("v_cvt_pk_f16_f32 v[%2], %0, %1" : : "v"(lo), "v"(hi), "n"(R));
+}
 // v[R] = (lo, hi) rounded to nearest-even and packed; the packed pair's two values are added to acc
 template <typename T, int R>
 __device__ __forceinline__ void named_pack_and_sum(float lo, float hi, float &acc) {

@@ -1,0 +1,155 @@
+// Host launcher and C entry points of attention in a window (attn_kernel_window.h).
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include <algorithm>
+
+#include "attn_kernel_window.h"
+#include "calibatt.h"
+#include "launch.h"
+
+namespace {
+using namespace calibatt_dev;
+using namespace calibatt_host;
+
+constexpr int WINDOW_CUS = 256;        // plans are functions of the sizes alone
+constexpr int WINDOW_MAX_PARTS = 64;
+
+// Keys that n neighbouring queries see at most, without the sinks.
+int64_t window_span(const calibatt_window &w, int n, int Nk) {
+  if (w.left < 0 || w.right < 0) return Nk;
+  // their frames are at most (n - 1) / frame + 2
+  const int64_t frames = (int64_t)(n - 1) / w.frame + 2 + w.left + w.right;
+  return std::min<int64_t>(Nk, frames * w.frame);
+}
+int64_t window_tiles(const calibatt_window &w, int n, int Nk, int tile) {
+  return (std::min<int64_t>(w.sinks, Nk) + tile - 1) / tile + (window_span(w, n, Nk) + tile - 1) / tile;
+}
+
+// Few enough rows of queries to a key head to go through the kernel that reads keys once for all of them.
+bool is_step(int Hq, int Hkv, int Nq) { return (int64_t)(Hq / Hkv) * Nq <= 32; }
+
+// Pieces that the tiles of every block of queries are cut into.
+int forward_parts(int B, int Hq, int Hkv, int Nq, int Nk, const calibatt_window &w) {
+  if (is_step(Hq, Hkv, Nq)) {
+    const int64_t units = (int64_t)B * Hkv, tiles = window_tiles(w, Nq, Nk, STEP_KEYS);
+    if (tiles <= 4 * STEP_WAVES) return 1;  // a second launch costs more than the four rounds of the waves
+    const int64_t fill = std::max<int64_t>(1, 2 * WINDOW_CUS / units);
+    return (int)std::max<int64_t>(1, std::min<int64_t>({fill, (tiles + 2 * STEP_WAVES - 1) / (2 * STEP_WAVES), WINDOW_MAX_PARTS}));
+  }
+  const int64_t units = (int64_t)B * Hq * ((Nq + 127) / 128), tiles = window_tiles(w, 128, Nk, 64);
+  const int64_t fill = 2 * WINDOW_CUS / units;
+  return (int)std::max<int64_t>(1, std::min<int64_t>({fill, tiles / 6, WINDOW_MAX_PARTS}));
+}
+
+int64_t forward_bytes(int parts, int B, int Hq, int Nq, int D) {
+  return parts > 1 ? (int64_t)parts * B * Hq * Nq * (D + 2) * 4 : 0;
+}
+
+int window_check(int B, int Hq, int Hkv, int Nq, int Nk, int D, const calibatt_window &w) {
+  if (B <= 0 || Hq <= 0 || Hkv <= 0 || Nq <= 0 || Nk <= 0 || D <= 0 || Hq % Hkv) return CALIBATT_ERR_SHAPE;
+  if (Nq > 1 << 30 || Nk > 1 << 30 || w.left < -1 || w.right < -1 || w.sinks < 0 || w.frame <= 0) return CALIBATT_ERR_SHAPE;
+  if (w.offset > 1 << 30 || w.offset < -(1 << 30)) return CALIBATT_ERR_SHAPE;
+  if ((int64_t)B * Hq > 1 << 24 || (int64_t)B * Hq * Nq > 0x7fffffffLL || (int64_t)B * Hkv * Nk > 0x7fffffffLL) return CALIBATT_ERR_SHAPE;
+  if (((uintptr_t)w.q_start | (uintptr_t)w.q_len | (uintptr_t)w.k_len) & 3) return CALIBATT_ERR_SHAPE;
+  if (D != 64 && D != 128) return CALIBATT_ERR_UNSUPPORTED;
+  return CALIBATT_OK;
+}
+
+// Strides of a tensor; those of an axis of one entry are never stepped along.
+bool window_strides(const calibatt_strides *given, int B, int H, int N, int D, Strides &s) {
+  s = given ? Strides{given->b, given->h, given->n} : Strides{(int64_t)H * N * D, (int64_t)N * D, D};
+  if (B == 1) s.b = 0;
+  if (H == 1) s.h = 0;
+  if (N == 1) s.n = D;
+  if (s.n < D || s.b < 0 || s.h < 0 || s.n % 8 || s.h % 8 || s.b % 8) return false;
+  // rows of one head are addressed with 32-bit byte offsets
+  return (unsigned long long)(N - 1) * (unsigned long long)s.n * 2 + (unsigned long long)D * 2 <= 0xffffffffULL;
+}
+
+int window_dims(int B, int Hq, int Hkv, int Nq, int Nk, const calibatt_window &w, float scale, WindowDims &p) {
+  p = WindowDims{};
+  p.B = B;
+  p.Hq = Hq;
+  p.Hkv = Hkv;
+  p.Nq = Nq;
+  p.Nk = Nk;
+  p.left = w.left;
+  p.right = w.right;
+  p.sinks = std::min(w.sinks, Nk);
+  p.frame = w.frame;
+  p.offset = w.offset;
+  p.q_start = w.q_start;
+  p.q_len = w.q_len;
+  p.k_len = w.k_len;
+  p.scale = scale;
+  p.scale_log2e = scale * 1.4426950408889634f;
+  p.parts = 1;
+  return CALIBATT_OK;
+}
+
+template <int D, typename T>
+int launch_forward(const uint16_t *q, const uint16_t *k, const uint16_t *v, uint16_t *out, float *lse, const WindowDims &p,
+                   hipStream_t stream) {
+  const bool step = is_step(p.Hq, p.Hkv, p.Nq);
+  const int64_t units = (int64_t)p.B * (step ? p.Hkv : p.Hq * ((p.Nq + 127) / 128)) * p.parts;
+  if (units > 0x7ffffff0LL) return CALIBATT_ERR_SHAPE;
+  const unsigned grid = (unsigned)(8 * ((units + 7) / 8));
+  int unused = 0, st;
+  if (step) {
+    static DevInfo info;
+    constexpr int SMEM = StepLds<D, T>::BYTES;
+    if ((st = prepare(window_attn_step_kernel<D, T>, STEP_WAVES * 64, SMEM, info, unused))) return st;
+    st = launch_kernel(window_attn_step_kernel<D, T>, grid, STEP_WAVES * 64, SMEM, stream, q, k, v, out, lse, p);
+  } else {
+    static DevInfo info;
+    constexpr int SMEM = WindowRow<D, T>::LDS_BYTES;
+    if ((st = prepare(window_attn_fwd_kernel<D, T>, 256, SMEM, info, unused))) return st;
+    st = launch_kernel(window_attn_fwd_kernel<D, T>, grid, 256, SMEM, stream, q, k, v, out, lse, p);
+  }
+  if (st || p.parts == 1) return st;
+  const int64_t rows = (int64_t)p.B * p.Hq * p.Nq, per_wg = 256 / (D / 8);
+  return launch_kernel(window_attn_merge_kernel<D, T>, (unsigned)((rows + per_wg - 1) / per_wg), 256, 0, stream, out, lse, p);
+}
+
+}  // namespace
+
+extern "C" int calibatt_window_attn_workspace_bytes(int B, int Hq, int Hkv, int Nq, int Nk, int D,
+                                                    const calibatt_window *window, int64_t *forward) {
+  if (!window || !forward) return CALIBATT_ERR_NULL;
+  if (int st = window_check(B, Hq, Hkv, Nq, Nk, D, *window)) return st;
+  *forward = forward_bytes(forward_parts(B, Hq, Hkv, Nq, Nk, *window), B, Hq, Nq, D);
+  return CALIBATT_OK;
+}
+
+extern "C" int calibatt_window_attn_fwd(const void *q, const void *k, const void *v, void *out, float *lse, int B, int Hq,
+                                        int Hkv, int Nq, int Nk, int D, const calibatt_window *window, float scale,
+                                        const calibatt_strides *q_strides, const calibatt_strides *kv_strides,
+                                        const calibatt_strides *out_strides, int dtype, void *workspace,
+                                        int64_t workspace_bytes, void *stream) {
+  if (!q || !k || !v || !out || !window) return CALIBATT_ERR_NULL;
+  if (int st = window_check(B, Hq, Hkv, Nq, Nk, D, *window)) return st;
+  if (dtype != CALIBATT_BF16 && dtype != CALIBATT_F16) return CALIBATT_ERR_UNSUPPORTED;
+  if (out == q || out == k || out == v || !(scale - scale == 0.f)) return CALIBATT_ERR_SHAPE;
+  WindowDims p;
+  window_dims(B, Hq, Hkv, Nq, Nk, *window, scale, p);
+  if (!window_strides(q_strides, B, Hq, Nq, D, p.q) || !window_strides(kv_strides, B, Hkv, Nk, D, p.kv) ||
+      !window_strides(out_strides, B, Hq, Nq, D, p.out))
+    return CALIBATT_ERR_SHAPE;
+  if ((((uintptr_t)q | (uintptr_t)k | (uintptr_t)v | (uintptr_t)out | (uintptr_t)workspace) & 15) || ((uintptr_t)lse & 3))
+    return CALIBATT_ERR_SHAPE;
+  if (workspace) {
+    p.parts = forward_parts(B, Hq, Hkv, Nq, Nk, *window);
+    if (workspace_bytes < forward_bytes(p.parts, B, Hq, Nq, D)) return CALIBATT_ERR_BUFFER_TOO_SMALL;
+    p.part_rows = (float *)workspace;
+    p.part_ml = p.part_rows + (size_t)p.parts * B * Hq * Nq * D;
+  }
+  const uint16_t *const q_ = (const uint16_t *)q, *const k_ = (const uint16_t *)k, *const v_ = (const uint16_t *)v;
+  uint16_t *const o_ = (uint16_t *)out;
+  hipStream_t s = (hipStream_t)stream;
+  if (D == 128)
+    return dtype == CALIBATT_BF16 ? launch_forward<128, Bf16>(q_, k_, v_, o_, lse, p, s)
+                                  : launch_forward<128, F16>(q_, k_, v_, o_, lse, p, s);
+  return dtype == CALIBATT_BF16 ? launch_forward<64, Bf16>(q_, k_, v_, o_, lse, p, s)
+                                : launch_forward<64, F16>(q_, k_, v_, o_, lse, p, s);
+}

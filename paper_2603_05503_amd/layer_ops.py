@@ -37,6 +37,11 @@ def declare(lib):
     lib.calibatt_layer_norm_bwd.restype = C.c_int
     lib.calibatt_layer_norm_bwd.argtypes = [C.c_void_p] * 6 + [C.c_int64] * 3 + [C.c_int] + [C.c_void_p] * 3 + [
         C.c_float, C.c_int, C.c_int, C.c_int, C.c_void_p, C.c_int64, C.c_void_p]
+    lib.calibatt_window_attn_workspace_bytes.restype = C.c_int
+    lib.calibatt_window_attn_workspace_bytes.argtypes = [C.c_int] * 6 + [C.c_void_p, i64p]
+    lib.calibatt_window_attn_fwd.restype = C.c_int
+    lib.calibatt_window_attn_fwd.argtypes = [C.c_void_p] * 5 + [C.c_int] * 6 + [C.c_void_p, C.c_float] + [C.c_void_p] * 3 + [
+        C.c_int, C.c_void_p, C.c_int64, C.c_void_p]
 
 
 _dtypes = None
@@ -277,3 +282,107 @@ def layer_norm_bwd(dy, x, weight=None, bias=None, eps: float = 1e-6, center: boo
     if st != 0:
         raise _b.CalibattError(st, "calibatt_layer_norm_bwd")
     return to, dweight, dbias
+
+
+class _CWindow(C.Structure):
+    _fields_ = [("left", C.c_int32), ("right", C.c_int32), ("sinks", C.c_int32), ("frame", C.c_int32), ("offset", C.c_int32),
+                ("q_start", C.c_void_p), ("q_len", C.c_void_p), ("k_len", C.c_void_p)]
+
+
+class Window:
+    """Which keys a query sees (``calibatt_window``): those of ``left`` frames before its own to ``right`` frames behind it
+    (-1: all), and the first ``sinks`` keys that are not ahead of that.  ``frame``: tokens of a frame (1: a window of
+    tokens).  ``offset``: position of the first query, for calls without ``q_start``: ``Nk - Nq`` where the queries are the
+    last of the keys."""
+
+    def __init__(self, left: int, right: int = 0, sinks: int = 0, frame: int = 1, offset: int = 0):
+        values = dict(left=left, right=right, sinks=sinks, frame=frame, offset=offset)
+        for name, v in values.items():
+            if not -(2 ** 31) <= int(v) < 2 ** 31:
+                raise ValueError(f"{name} does not fit 32 bits")
+        self.left, self.right, self.sinks, self.frame, self.offset = (int(v) for v in values.values())
+        self._bytes = {}  # sizes of a call -> workspace bytes of its forward
+
+    def _c(self, q_start, q_len, k_len, B, device):
+        """The C struct of one call."""
+        import torch
+
+        c = _CWindow(self.left, self.right, self.sinks, self.frame, self.offset)
+        for name, t in (("q_start", q_start), ("q_len", q_len), ("k_len", k_len)):
+            if t is not None:
+                if not (t.device == device and t.dtype == torch.int32 and t.dim() == 1 and t.shape[0] == B and t.is_contiguous()):
+                    raise ValueError(f"{name} must be a contiguous int32 CUDA tensor with one entry per batch entry")
+                setattr(c, name, t.data_ptr())
+        return c
+
+    def workspace_bytes(self, B: int, Hq: int, Hkv: int, Nq: int, Nk: int, D: int):
+        """calibatt_window_attn_workspace_bytes."""
+        key = (B, Hq, Hkv, Nq, Nk, D)
+        n = self._bytes.get(key)
+        if n is None:
+            c, got = _CWindow(self.left, self.right, self.sinks, self.frame, self.offset), C.c_int64(0)
+            st = _b.load_library().calibatt_window_attn_workspace_bytes(*key, C.addressof(c), C.byref(got))
+            if st != 0:
+                raise _b.CalibattError(st, "calibatt_window_attn_workspace_bytes")
+            if len(self._bytes) >= 256:
+                self._bytes.clear()
+            n = self._bytes[key] = got.value
+        return n
+
+
+def _window_tensors(q, k, v, like_q):
+    """Checks the tensors of a call; (B, Hq, Nq, D, Hkv, Nk, dtype)."""
+    dtype = _dtype_of(q)
+    if not (q.is_cuda and dtype in (0, 1) and q.dim() == 4 and q.stride(3) == 1):
+        raise ValueError("q must be a bf16 or fp16 CUDA tensor [B, H, N, D] with contiguous D")
+    B, Hq, Nq, D = q.shape
+    for name, t in like_q:
+        if not (t.shape == q.shape and t.dtype == q.dtype and t.device == q.device and t.stride(3) == 1):
+            raise ValueError(f"{name} must have the shape, element type and device of q, with contiguous D")
+    for t in (k, v):
+        if not (t.dim() == 4 and t.dtype == q.dtype and t.device == q.device and t.stride(3) == 1
+                and t.shape[0] == B and t.shape[3] == D):
+            raise ValueError("k and v must be [B, Hkv, Nk, D] of q's element type and device, with contiguous D")
+    if k.shape != v.shape or k.stride() != v.stride():
+        raise ValueError("k and v must share their shape and strides")
+    if k.shape[1] == 0 or Hq % k.shape[1]:
+        raise ValueError("the query heads must be a multiple of the key heads")
+    return B, Hq, Nq, D, k.shape[1], k.shape[2], dtype
+
+
+def _check_lse(lse, q):
+    import torch
+
+    if not (lse.dtype == torch.float32 and lse.device == q.device and lse.shape == q.shape[:3] and lse.is_contiguous()):
+        raise ValueError("lse must be a contiguous fp32 CUDA tensor [B, H, N] on q's device")
+
+
+def window_attn_fwd(q, k, v, out, window: Window, scale: float, lse=None, q_start=None, q_len=None, k_len=None, stream=None):
+    """calibatt_window_attn_fwd on bf16 or fp16 CUDA tensors: q, out [B, Hq, Nq, D], k, v [B, Hkv, Nk, D] (views with
+    contiguous D; k and v share their strides; Hq a multiple of Hkv).  ``lse``: optional contiguous fp32 CUDA tensor [B,
+    Hq, Nq].  ``q_start``, ``q_len``, ``k_len``: optional int32 CUDA tensors [B]: position of a batch entry's first query,
+    how many queries and keys it has; rows behind these lengths may hold anything, their outputs are zeros.  Cut along the
+    keys where a few rows of queries would not fill the GPU, with a workspace of the call's own."""
+    import torch
+
+    lib = _b.load_library()
+    B, Hq, Nq, D, Hkv, Nk, dtype = _window_tensors(q, k, v, (("out", out),))
+    if lse is not None:
+        _check_lse(lse, q)
+    stream, other = _b._stream_of(stream, q.device)
+    c = window._c(q_start, q_len, k_len, B, q.device)
+    with _on(q.device):
+        nbytes, workspace = window.workspace_bytes(B, Hq, Hkv, Nq, Nk, D), None
+        if nbytes:
+            try:
+                workspace = _b._empty(nbytes // 4, torch.float32, q.device, other)
+            except torch.OutOfMemoryError:
+                pass  # whole rows, which take none
+        keep, at = _strides(q, k, out)
+        st = lib.calibatt_window_attn_fwd(q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(),
+                                          None if lse is None else lse.data_ptr(), B, Hq, Hkv, Nq, Nk, D, C.addressof(c),
+                                          float(scale), *at, dtype, None if workspace is None else workspace.data_ptr(),
+                                          nbytes, stream)
+    if st != 0:
+        raise _b.CalibattError(st, "calibatt_window_attn_fwd")
+    return out

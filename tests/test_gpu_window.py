@@ -1,0 +1,196 @@
+"""GPU tests of attention in a window with first tokens that stay visible, against the fp64 oracle.
+
+Tolerances of the forward: the probabilities and the result are each rounded to the element type, half a step at most,
+relative to the probability and to the value.  An output off by both is within half a step of sum_j p_j |v_j| and half a
+step of itself; fp32 sums and exponentials add 2^-24 times the number of keys' logits, which is far below (counted as
+2^-14 of sum_j p_j |v_j|: logits of up to 2^6 with 2^-24 each, 2^8 roundings in a row).  The log-sum-exp is fp32: logits
+of up to 2^6 in log2 units, and sums of positive numbers, 2^-24 * (2^8 + |lse| 2^2)."""
+import math
+
+import numpy as np
+import pytest
+
+from oracle import layer
+
+pytestmark = pytest.mark.gpu
+
+U = 2.0 ** -24
+
+
+def _torch():
+    import torch
+
+    return torch
+
+
+def make(rng, shape, dtype, gain=1.0):
+    torch = _torch()
+    return torch.from_numpy((gain * rng.standard_normal(shape)).astype(np.float32)).cuda().to(getattr(torch, dtype))
+
+
+def laid_out(x, layout):
+    """The same values in another memory layout, between rows of NaN."""
+    torch = _torch()
+    B, H, N, D = x.shape
+    if layout == "packed":
+        return x.clone()
+    if layout == "bnhd":
+        buf = torch.full((B, N + 3, H, D), float("nan"), dtype=x.dtype, device=x.device)
+        view = buf[:, 1:N + 1].transpose(1, 2)
+    else:  # one of three neighbours in a fused projection
+        buf = torch.full((B, N + 2, 3, H, D), float("nan"), dtype=x.dtype, device=x.device)
+        view = buf[:, 1:N + 1, 1].transpose(1, 2)
+    view.copy_(x)
+    return view
+
+
+def f64(t):
+    return t.double().cpu().numpy()
+
+
+def visible(c, B, Nq, Nk, start=None, q_len=None, k_len=None):
+    return np.stack([layer.window_visible(Nq, Nk, c["left"], c["right"], c["sinks"], c["frame"],
+                                          c.get("offset", 0) if start is None else start[b],
+                                          None if q_len is None else q_len[b], None if k_len is None else k_len[b])
+                     for b in range(B)])
+
+
+def check_forward(out, lse, q, k, v, see, scale, dtype):
+    torch = _torch()
+    half = 0.5 * torch.finfo(getattr(torch, dtype)).eps
+    qs, ks, vs = f64(q), f64(k), f64(v)
+    want, want_lse = layer.window_attention(qs, ks, vs, see, scale)
+    size, _ = layer.window_attention(qs, ks, np.abs(vs), see, scale)
+    got = f64(out)
+    allowed = half * 1.01 * (np.abs(want) + size) + 2.0 ** -14 * size + 1e-7
+    off = np.abs(got - want) / allowed
+    assert np.isfinite(got).all() and off.max() <= 1.0, f"out: worst {off.max():.2f} of what is allowed"
+    empty = ~np.isfinite(want_lse)
+    assert (got[empty] == 0).all()
+    if lse is not None:
+        z = f64(lse)
+        assert np.array_equal(np.isneginf(z), empty)
+        off = np.abs(z - want_lse)[~empty] / (U * (2 ** 8 + 4 * np.abs(want_lse[~empty])))
+        assert off.size == 0 or off.max() <= 1.0, f"lse: worst {off.max():.2f} of what is allowed"
+
+
+# B, Hq, Hkv, Nq, Nk, D, window
+CASES = [
+    (1, 2, 2, 1, 1, 64, dict(left=0, right=0, sinks=0, frame=1)),
+    (2, 4, 2, 130, 130, 128, dict(left=-1, right=0, sinks=0, frame=1)),
+    (1, 3, 3, 300, 300, 128, dict(left=40, right=0, sinks=4, frame=1)),
+    (1, 2, 1, 517, 517, 64, dict(left=60, right=13, sinks=70, frame=1)),
+    (1, 2, 2, 6 * 77, 6 * 77, 128, dict(left=1, right=0, sinks=77, frame=77)),
+    (2, 2, 2, 5 * 150, 5 * 150, 64, dict(left=1, right=1, sinks=33, frame=150)),
+    (1, 1, 1, 1000, 1000, 128, dict(left=0, right=0, sinks=200, frame=1)),
+    (1, 2, 2, 700, 700, 128, dict(left=-1, right=-1, sinks=0, frame=1)),
+    (1, 2, 2, 260, 900, 128, dict(left=100, right=0, sinks=10, frame=1, offset=640)),
+    (1, 2, 2, 260, 900, 64, dict(left=2, right=-1, sinks=0, frame=64, offset=300)),
+    (1, 2, 2, 400, 200, 128, dict(left=30, right=0, sinks=0, frame=1, offset=-100)),  # queries before and behind all keys
+    (1, 2, 2, 400, 200, 64, dict(left=3, right=1, sinks=6, frame=16, offset=-150)),
+    (1, 40, 40, 129, 65, 128, dict(left=-1, right=-1, sinks=0, frame=1)),
+    # few rows of queries: single tokens, shared key heads
+    (3, 8, 2, 1, 700, 64, dict(left=256, right=0, sinks=4, frame=1, offset=699)),
+    (2, 16, 2, 1, 5000, 128, dict(left=-1, right=0, sinks=0, frame=1, offset=4999)),
+    (1, 4, 4, 1, 33, 128, dict(left=10, right=0, sinks=3, frame=1, offset=32)),
+    (2, 8, 1, 4, 3001, 128, dict(left=1000, right=0, sinks=70, frame=1, offset=2997)),
+    (1, 2, 2, 32, 2100, 64, dict(left=500, right=0, sinks=0, frame=7, offset=2068)),
+    (1, 4, 2, 3, 900, 64, dict(left=5, right=0, sinks=0, frame=100, offset=-2)),
+]
+
+
+@pytest.mark.parametrize("B,Hq,Hkv,Nq,Nk,D,c", CASES)
+@pytest.mark.parametrize("dtype,layout", [("bfloat16", "packed"), ("float16", "bnhd"), ("bfloat16", "fused")])
+def test_window_forward(lib, B, Hq, Hkv, Nq, Nk, D, c, dtype, layout):
+    torch = _torch()
+    print(f"window {B} {Hq} {Hkv} {Nq} {Nk} {D} {c} {dtype} {layout}", flush=True)
+    rng = np.random.default_rng(Nq + Nk)
+    q, k, v = make(rng, (B, Hq, Nq, D), dtype, 1.5), make(rng, (B, Hkv, Nk, D), dtype, 1.5), make(rng, (B, Hkv, Nk, D), dtype)
+    scale = 1 / math.sqrt(D)
+    out, lse = laid_out(torch.full_like(q, 7.0), layout), torch.full((B, Hq, Nq), 7.0, device="cuda")
+    w = lib.Window(**c)
+    args = [laid_out(t, layout) for t in (q, k, v)]
+    assert lib.window_attn_fwd(*args, out, w, scale, lse=lse) is out
+    check_forward(out, lse, q, k, v, visible(c, B, Nq, Nk), scale, dtype)
+    again = torch.empty_like(q)
+    lib.window_attn_fwd(q, k, v, again, w, scale)
+    assert torch.equal(again, out)  # the same bits whatever the layout, with and without lse
+
+
+LENGTHS = [
+    # B, Hq, Hkv, Nq, Nk, D, window, start, q_len, k_len
+    (4, 2, 2, 300, 300, 128, dict(left=64, right=0, sinks=5, frame=1), [0, 0, 0, 0], [300, 0, 131, 1], [300, 0, 131, 1]),
+    (3, 4, 2, 200, 640, 64, dict(left=2, right=1, sinks=40, frame=50), [440, 17, 0], [200, 128, 129], [640, 145, 3]),
+    (3, 2, 1, 150, 400, 128, dict(left=-1, right=-1, sinks=0, frame=1), [0, 5, 9], [150, 150, 7], [0, 400, 399]),
+    (5, 8, 2, 1, 4096, 128, dict(left=1023, right=0, sinks=16, frame=1), [4095, -1, 0, 999, 2500], [1, 0, 1, 1, 1], [4096, 0, 1, 1000, 2501]),
+    (3, 4, 4, 3, 777, 64, dict(left=-1, right=0, sinks=0, frame=1), [774, 100, -5], [3, 2, 3], [777, 102, 777]),
+    # lengths that are not lengths, positions beyond all measure
+    (4, 2, 2, 130, 200, 64, dict(left=20, right=0, sinks=3, frame=1), [70, 2 ** 31 - 1, -(2 ** 31), 0], [1000, 130, 130, -7], [2 ** 31 - 1, 200, 200, 200]),
+]
+
+
+@pytest.mark.parametrize("B,Hq,Hkv,Nq,Nk,D,c,start,q_len,k_len", LENGTHS)
+@pytest.mark.parametrize("dtype", ["bfloat16", "float16"])
+def test_window_forward_with_lengths(lib, B, Hq, Hkv, Nq, Nk, D, c, start, q_len, k_len, dtype):
+    """Padded batches; behind a sequence's end, and where no query sees, there is NaN."""
+    torch = _torch()
+    print(f"lengths {B} {Nq} {Nk} {D} {c} {start} {q_len} {k_len} {dtype}", flush=True)
+    rng = np.random.default_rng(B + Nk)
+    q, k, v = make(rng, (B, Hq, Nq, D), dtype), make(rng, (B, Hkv, Nk, D), dtype), make(rng, (B, Hkv, Nk, D), dtype)
+    see = visible(c, B, Nq, Nk, np.clip(start, -(2 ** 30), 2 ** 30), q_len, k_len)
+    scale, nan = 0.11, float("nan")
+    qn, kn, vn = q.clone(), k.clone(), v.clone()
+    for b in range(B):
+        qn[b, :, max(0, q_len[b]):] = nan
+        unseen = torch.from_numpy(~see[b].any(0)).cuda()
+        kn[b, :, unseen] = nan
+        vn[b, :, unseen] = float("inf")
+    at = [torch.tensor(np.array(x, dtype=np.int64).astype(np.int32), device="cuda") for x in (start, q_len, k_len)]
+    out, lse = torch.full_like(q, 7.0), torch.full((B, Hq, Nq), 7.0, device="cuda")
+    lib.window_attn_fwd(qn, kn, vn, out, lib.Window(**c), scale, lse=lse, q_start=at[0], q_len=at[1], k_len=at[2])
+    check_forward(out, lse, q, k, v, see, scale, dtype)
+
+
+@pytest.mark.parametrize("Nq", [1, 200])
+@pytest.mark.parametrize("gain", [1.0, 30.0])
+def test_window_large_logits_and_any_scale(lib, Nq, gain):
+    """Rows that one key takes, negative and zero scales."""
+    torch = _torch()
+    rng = np.random.default_rng(3)
+    q, k, v = (make(rng, (1, 2, n, 128), "bfloat16", g) for n, g in ((Nq, gain), (500, 1.0), (500, 1.0)))
+    c = dict(left=300, right=0, sinks=9, frame=1, offset=500 - Nq)
+    for scale in (1 / math.sqrt(128), -1 / math.sqrt(128), 0.0):
+        out = torch.empty_like(q)
+        lib.window_attn_fwd(q, k, v, out, lib.Window(**c), scale)
+        half = 2.0 ** -8
+        want, _ = layer.window_attention(f64(q), f64(k), f64(v), visible(c, 1, Nq, 500), scale)
+        size, _ = layer.window_attention(f64(q), f64(k), np.abs(f64(v)), visible(c, 1, Nq, 500), scale)
+        # logits of up to 30 * 128 / sqrt(128) * 4 = 2^10.4 in fp32: exponents off by 2^-24 * 2^11 * 2^2 from 128 products
+        assert (np.abs(f64(out) - want) <= half * 1.01 * (np.abs(want) + size) + 2.0 ** -10 * size + 1e-7).all()
+
+
+def test_window_refusals(lib):
+    torch = _torch()
+    q = torch.zeros((2, 4, 64, 64), dtype=torch.bfloat16, device="cuda")
+    k, out, w = torch.zeros((2, 2, 96, 64), dtype=torch.bfloat16, device="cuda"), torch.empty_like(q), lib.Window(4)
+    one = torch.zeros(2, dtype=torch.int32, device="cuda")
+    f = lib.window_attn_fwd
+    for call in (lambda: f(q.float(), k, k, out, w, 1.0), lambda: f(q, k.half(), k, out, w, 1.0), lambda: f(q, k, k[:, :, :64], out, w, 1.0),
+                 lambda: f(q, k, k.transpose(1, 2).contiguous().transpose(1, 2), out, w, 1.0), lambda: f(q[:, :3], k, k, out[:, :3], w, 1.0),
+                 lambda: f(q, k[:1], k[:1], out, w, 1.0), lambda: f(q, k, k, out[:, :, :32], w, 1.0), lambda: f(q, k, k, out.half(), w, 1.0),
+                 lambda: f(q, k, k, out, w, 1.0, lse=torch.zeros((2, 4, 64), device="cuda").half()),
+                 lambda: f(q, k, k, out, w, 1.0, lse=torch.zeros((2, 64, 4), device="cuda").transpose(1, 2)),
+                 lambda: f(q, k, k, out, w, 1.0, q_len=one.long()), lambda: f(q, k, k, out, w, 1.0, k_len=one[:1]),
+                 lambda: f(q, k, k, out, w, 1.0, q_start=one.cpu()), lambda: f(q[0], k, k, out, w, 1.0), lambda: f(q.cpu(), k, k, out, w, 1.0)):
+        with pytest.raises(ValueError):
+            call()
+    for call in (lambda: f(q, k, k, out, lib.Window(-2), 1.0), lambda: f(q, k, k, out, lib.Window(1, -2), 1.0),
+                 lambda: f(q, k, k, out, lib.Window(1, sinks=-1), 1.0), lambda: f(q, k, k, out, lib.Window(1, frame=0), 1.0),
+                 lambda: f(q, k, k, q, w, 1.0), lambda: f(q, k, k, out, w, math.inf), lambda: f(q, k, k, out, w, math.nan),
+                 lambda: f(q[..., :32], k[..., :32], k[..., :32], out[..., :32], w, 1.0), lambda: f(q, k, k, out, lib.Window(1, offset=2 ** 30 + 1), 1.0),
+                 lambda: f(q.expand(2, 4, 64, 64)[:, :, :1].expand(2, 4, 64, 64), k, k, out, w, 1.0)):
+        with pytest.raises(lib.CalibattError):
+            call()
+    with pytest.raises(ValueError):
+        lib.Window(2 ** 31)
+    torch.cuda.synchronize()

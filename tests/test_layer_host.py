@@ -126,3 +126,46 @@ def test_oracle_rope_gradient_is_the_inverse():
         y = layer.rope(x, *args)
         assert np.allclose(layer.rope(y, *args, inverse=True), x, atol=1e-13)
         assert abs((y * dy).sum() - (x * layer.rope(dy, *args, inverse=True)).sum()) < 1e-12
+
+
+# ---- attention in a window: refusals, and sizes of workspaces ------------------------------------------------
+def _window(fn="bytes", B=2, Hq=4, Hkv=2, Nq=300, Nk=300, D=64, left=10, right=0, sinks=0, frame=1, offset=0, q_start=None, q=P, k=P,
+            v=P, out=2 * P, lse=P, scale=1.0, dtype=0, sq=None, skv=None, so=None, ws=None, nbytes=0):
+    from paper_2603_05503_amd.layer_ops import _CWindow
+
+    w = _CWindow(left, right, sinks, frame, offset, q_start, None, None)
+    lib = pkg.load_library()
+    if fn == "bytes":
+        n = C.c_int64(-1)
+        st = lib.calibatt_window_attn_workspace_bytes(B, Hq, Hkv, Nq, Nk, D, C.addressof(w), C.byref(n))
+        return st if st else n.value
+    arrays = [None if s is None else (C.c_int64 * 3)(*s) for s in (sq, skv, so)]
+    return lib.calibatt_window_attn_fwd(q, k, v, out, lse, B, Hq, Hkv, Nq, Nk, D, C.addressof(w), scale,
+                                        *(None if a is None else C.addressof(a) for a in arrays), dtype, ws, nbytes, None)
+
+
+@pytest.mark.parametrize("kw,status", [
+    (dict(B=0), SHAPE), (dict(Hq=3), SHAPE), (dict(Hkv=0), SHAPE), (dict(Nq=0), SHAPE), (dict(Nk=-1), SHAPE), (dict(D=96), UNSUPPORTED),
+    (dict(left=-2), SHAPE), (dict(right=-2), SHAPE), (dict(sinks=-1), SHAPE), (dict(frame=0), SHAPE), (dict(offset=-(1 << 30) - 1), SHAPE),
+    (dict(q_start=P + 2), SHAPE), (dict(B=1 << 12, Nq=1 << 20), SHAPE), (dict(B=1 << 12, Nk=1 << 19), SHAPE)])
+def test_window_size_refusals(kw, status):
+    assert _window(**kw) == status
+    assert _window("fwd", **kw) == status
+
+
+@pytest.mark.parametrize("kw,status", [
+    (dict(q=None), NULL), (dict(k=None), NULL), (dict(v=None), NULL), (dict(out=None), NULL), (dict(out=P), SHAPE),
+    (dict(scale=math.inf), SHAPE), (dict(scale=math.nan), SHAPE), (dict(dtype=2), UNSUPPORTED), (dict(q=P + 8), SHAPE),
+    (dict(lse=P + 2), SHAPE), (dict(sq=(1 << 20, 1 << 14, 60)), SHAPE), (dict(skv=(1 << 20, 1 << 14, 68)), SHAPE),
+    (dict(so=(-8, 1 << 14, 64)), SHAPE), (dict(skv=(0, 0, 1 << 24)), SHAPE), (dict(ws=P, nbytes=0, Nk=4096, left=-1), TOO_SMALL)])
+def test_window_forward_refusals(kw, status):
+    assert _window("fwd", **kw) == status
+
+
+def test_window_workspace_follows_the_work():
+    assert _window(Nq=32760, Nk=32760, Hq=40, Hkv=40) == 0                       # fills the GPU by itself
+    few = _window(B=1, Hq=1, Hkv=1, Nq=128, Nk=32760, left=-1)
+    assert few > 0 and few % ((64 + 2) * 4 * 128) == 0 and few // ((64 + 2) * 4 * 128) <= 64
+    assert _window(B=1, Hq=8, Hkv=2, Nq=1, Nk=100, left=-1) == 0                 # one short stream: one launch
+    assert _window(B=1, Hq=8, Hkv=2, Nq=1, Nk=1 << 20, left=-1) > 0
+    assert _window(B=1, Hq=8, Hkv=2, Nq=1, Nk=1 << 20, left=300) == 0            # by what is seen, not by the cache
