@@ -833,12 +833,34 @@ typedef struct calibatt_window {
  * UNSUPPORTED (D, dtype); BUFFER_TOO_SMALL; LAUNCH.
  */
 int calibatt_window_attn_workspace_bytes(int B, int Hq, int Hkv, int Nq, int Nk, int D,
-                                         const calibatt_window *window, int64_t *forward);
+                                         const calibatt_window *window, int64_t *forward,
+                                         int64_t *backward);
 int calibatt_window_attn_fwd(const void *q, const void *k, const void *v, void *out, float *lse, int B,
                              int Hq, int Hkv, int Nq, int Nk, int D, const calibatt_window *window,
                              float scale, const calibatt_strides *q_strides,
                              const calibatt_strides *kv_strides, const calibatt_strides *out_strides,
                              int dtype, void *workspace, int64_t workspace_bytes, void *stream);
+
+/*
+ * calibatt_window_attn_bwd: its gradients, for dout [B][Hq][Nq][D], the gradient
+ * of out: dq like q, dk and dv [B][Hkv][Nk][D] (summed over the query heads that
+ * share a key head; zeros for queries and keys that are not there or meet
+ * nothing).  out and lse are the forward's for the same arguments.  S and dP are
+ * formed twice, so that nothing is added up by atomics: the same inputs give the
+ * same bits.  Sums are fp32; the probabilities and dS are rounded to the element
+ * type for the products (fp16: times 2^15 and 2^4, dS may be up to 2^12).
+ * workspace: DEVICE, 16-byte aligned, calibatt_window_attn_workspace_bytes
+ * (`backward`), needed always.  No result may be an input.
+ * Errors: as calibatt_window_attn_fwd.
+ */
+int calibatt_window_attn_bwd(const void *dout, const void *q, const void *k, const void *v,
+                             const void *out, const float *lse, void *dq, void *dk, void *dv, int B,
+                             int Hq, int Hkv, int Nq, int Nk, int D, const calibatt_window *window,
+                             float scale, const calibatt_strides *dout_strides,
+                             const calibatt_strides *q_strides, const calibatt_strides *kv_strides,
+                             const calibatt_strides *out_strides, const calibatt_strides *dq_strides,
+                             const calibatt_strides *dkv_strides, int dtype, void *workspace,
+                             int64_t workspace_bytes, void *stream);
 
 /* Static, NUL-terminated description of a status code. */
 const char *calibatt_strerror(int status);

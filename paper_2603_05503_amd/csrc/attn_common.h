@@ -170,6 +170,10 @@ struct Bf16 {
     t[1] = (__bf16)hi;
     return __builtin_bit_cast(uint32_t, t);
   }
+  static __device__ __forceinline__ void unpack(uint32_t pk, float (&x)[2]) {
+    x[0] = __builtin_bit_cast(float, pk << 16);
+    x[1] = __builtin_bit_cast(float, pk & 0xffff0000u);
+  }
   static __device__ __forceinline__ float add_pair(uint32_t pk, float acc) {
     return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, pk), __builtin_bit_cast(bf16x2, 0x3f803f80u), acc, false);
   }
@@ -183,6 +187,11 @@ struct F16 {
     t[0] = (_Float16)lo;
     t[1] = (_Float16)hi;
     return __builtin_bit_cast(uint32_t, t);
+  }
+  static __device__ __forceinline__ void unpack(uint32_t pk, float (&x)[2]) {
+    const f16x2 two = __builtin_bit_cast(f16x2, pk);
+    x[0] = (float)two[0];
+    x[1] = (float)two[1];
   }
   static __device__ __forceinline__ float add_pair(uint32_t pk, float acc) {
     return __builtin_amdgcn_fdot2(__builtin_bit_cast(f16x2, pk), __builtin_bit_cast(f16x2, 0x3c003c00u), acc, false);

@@ -33,9 +33,9 @@ struct WindowEntry {
   int start, q_len, k_len;
   __device__ __forceinline__ WindowEntry(const WindowDims &p, int b) {
     // positions within 2^30 either way: differences and sums with lengths stay in 32 bits
-    start = min(max(p.q_start ? p.q_start[b] : p.offset, -(1 << 30)), 1 << 30);
-    q_len = p.q_len ? min(max(p.q_len[b], 0), p.Nq) : p.Nq;
-    k_len = p.k_len ? min(max(p.k_len[b], 0), p.Nk) : p.Nk;
+    start = __builtin_amdgcn_readfirstlane(min(max(p.q_start ? p.q_start[b] : p.offset, -(1 << 30)), 1 << 30));
+    q_len = __builtin_amdgcn_readfirstlane(p.q_len ? min(max(p.q_len[b], 0), p.Nq) : p.Nq);
+    k_len = __builtin_amdgcn_readfirstlane(p.k_len ? min(max(p.k_len[b], 0), p.Nk) : p.Nk);
   }
   // [lo, hi) of query i
   __device__ __forceinline__ void interval(const WindowDims &p, int i, int &lo, int &hi) const {

@@ -5,6 +5,7 @@
 #include <algorithm>
 
 #include "attn_kernel_window.h"
+#include "attn_kernel_window_bwd.h"
 #include "calibatt.h"
 #include "launch.h"
 
@@ -112,13 +113,88 @@ int launch_forward(const uint16_t *q, const uint16_t *k, const uint16_t *v, uint
   return launch_kernel(window_attn_merge_kernel<D, T>, (unsigned)((rows + per_wg - 1) / per_wg), 256, 0, stream, out, lse, p);
 }
 
+// ---- gradients ----------------------------------------------------------------------------------------------
+// How the gradients' kernels are cut: blocks of 32 columns per wave of either kernel, and the parts that the queries of a
+// block of keys are cut into.  A block with sinks is seen by all later queries, so it gets parts as long as the others'.
+struct GradPlan {
+  int nb_q, nb_k, parts, sink_parts, sink_blocks;
+  int64_t bytes;  // of the workspace: delta, and the sums of the parts
+};
+GradPlan grad_plan(int B, int Hq, int Hkv, int Nq, int Nk, int D, const calibatt_window &w) {
+  GradPlan g;
+  g.nb_q = (int64_t)B * Hq * ((Nq + 255) / 256) >= WINDOW_CUS ? 2 : 1;
+  g.nb_k = (int64_t)B * Hkv * ((Nk + 255) / 256) >= WINDOW_CUS / 2 ? 2 : 1;
+  const int block = 128 * g.nb_k, blocks = (Nk + block - 1) / block;
+  g.sink_blocks = w.left < 0 ? 0 : (std::min(w.sinks, Nk) + block - 1) / block;
+  const int64_t G = Hq / Hkv, heads = (int64_t)B * Hkv;
+  const int64_t all = G * ((Nq + 63) / 64);
+  int64_t one = all;  // tiles of queries that see a block, without sinks
+  if (w.left >= 0 && w.right >= 0) one = std::min<int64_t>(all, G * (window_span(w, block, Nq) + 63) / 64);
+  const int64_t total = heads * (g.sink_blocks * all + (blocks - g.sink_blocks) * one);
+  const int64_t slots = WINDOW_CUS * (g.nb_k == 2 ? 1 : 2);
+  // a third of an even share, so that the last parts end close to each other, but no short ones
+  const int64_t length = std::max<int64_t>({1, std::min<int64_t>(16, one), total / (3 * slots)});
+  g.parts = (int)std::min<int64_t>(WINDOW_MAX_PARTS, std::max<int64_t>(1, one / length));
+  g.sink_parts = (int)std::min<int64_t>(WINDOW_MAX_PARTS, std::max<int64_t>(1, all / std::max<int64_t>(1, one / g.parts)));
+  g.bytes = ((int64_t)B * Hq * Nq + 3) / 4 * 16;
+  const int64_t row = 2 * D * 4;
+  if (g.parts > 1) g.bytes += g.parts * heads * Nk * row;
+  if (g.sink_blocks && g.sink_parts > 1) g.bytes += g.sink_parts * heads * g.sink_blocks * block * row;
+  return g;
+}
+
+struct GradTensors {
+  const uint16_t *dout, *q, *k, *v, *out;
+  const float *lse;
+  uint16_t *dq, *dk, *dv;
+  float *delta;
+};
+
+template <int D, int NB, typename T>
+int launch_dq(const GradTensors &t, const WindowDims &p, hipStream_t stream) {
+  using Tile = GradTile<D, NB, T>;
+  static DevInfo info;
+  int unused = 0;
+  if (int st = prepare(window_attn_dq_kernel<D, NB, T>, 256, Tile::LDS_BYTES, info, unused)) return st;
+  const int64_t units = (int64_t)p.B * p.Hq * ((p.Nq + 128 * NB - 1) / (128 * NB));
+  return launch_kernel(window_attn_dq_kernel<D, NB, T>, (unsigned)(8 * ((units + 7) / 8)), 256, Tile::LDS_BYTES, stream, t.dout,
+                       t.q, t.k, t.v, t.out, t.lse, t.dq, t.delta, p);
+}
+
+template <int D, int NB, typename T>
+int launch_dkv(const GradTensors &t, const WindowDims &p, hipStream_t stream) {
+  using Tile = GradTile<D, NB, T>;
+  constexpr int SMEM = Tile::LDS_BYTES + 1024, BLOCK = 128 * NB;
+  static DevInfo info;
+  int unused = 0;
+  if (int st = prepare(window_attn_dkv_kernel<D, NB, T>, 256, SMEM, info, unused)) return st;
+  const int blocks = (p.Nk + BLOCK - 1) / BLOCK;
+  const int64_t units = (int64_t)p.B * p.Hkv * ((int64_t)p.n_sink_blocks * p.bwd_sink_parts + (int64_t)(blocks - p.n_sink_blocks) * p.bwd_parts);
+  if (units > 0x7ffffff0LL) return CALIBATT_ERR_SHAPE;
+  if (int st = launch_kernel(window_attn_dkv_kernel<D, NB, T>, (unsigned)(8 * ((units + 7) / 8)), 256, SMEM, stream, t.dout, t.q,
+                             t.k, t.v, t.lse, (const float *)t.delta, t.dk, t.dv, p))
+    return st;
+  const int64_t cut = p.bwd_parts > 1 ? p.Nk : p.bwd_sink_parts > 1 ? std::min(p.Nk, p.n_sink_blocks * BLOCK) : 0;
+  const int64_t rows = 2 * cut * p.B * p.Hkv, per_wg = 256 / (D / 8);
+  if (rows == 0) return CALIBATT_OK;
+  if ((rows + per_wg - 1) / per_wg > 0x7fffffff) return CALIBATT_ERR_SHAPE;
+  return launch_kernel(window_attn_dkv_sum_kernel<D, NB, T>, (unsigned)((rows + per_wg - 1) / per_wg), 256, 0, stream, t.dk, t.dv, p);
+}
+
+template <int D, typename T>
+int launch_backward(const GradTensors &t, const WindowDims &p, const GradPlan &g, hipStream_t stream) {
+  if (int st = g.nb_q == 2 ? launch_dq<D, 2, T>(t, p, stream) : launch_dq<D, 1, T>(t, p, stream)) return st;
+  return g.nb_k == 2 ? launch_dkv<D, 2, T>(t, p, stream) : launch_dkv<D, 1, T>(t, p, stream);
+}
+
 }  // namespace
 
 extern "C" int calibatt_window_attn_workspace_bytes(int B, int Hq, int Hkv, int Nq, int Nk, int D,
-                                                    const calibatt_window *window, int64_t *forward) {
-  if (!window || !forward) return CALIBATT_ERR_NULL;
+                                                    const calibatt_window *window, int64_t *forward, int64_t *backward) {
+  if (!window || !forward || !backward) return CALIBATT_ERR_NULL;
   if (int st = window_check(B, Hq, Hkv, Nq, Nk, D, *window)) return st;
   *forward = forward_bytes(forward_parts(B, Hq, Hkv, Nq, Nk, *window), B, Hq, Nq, D);
+  *backward = grad_plan(B, Hq, Hkv, Nq, Nk, D, *window).bytes;
   return CALIBATT_OK;
 }
 
@@ -152,4 +228,42 @@ extern "C" int calibatt_window_attn_fwd(const void *q, const void *k, const void
                                   : launch_forward<128, F16>(q_, k_, v_, o_, lse, p, s);
   return dtype == CALIBATT_BF16 ? launch_forward<64, Bf16>(q_, k_, v_, o_, lse, p, s)
                                 : launch_forward<64, F16>(q_, k_, v_, o_, lse, p, s);
+}
+
+extern "C" int calibatt_window_attn_bwd(const void *dout, const void *q, const void *k, const void *v, const void *out,
+                                        const float *lse, void *dq, void *dk, void *dv, int B, int Hq, int Hkv, int Nq, int Nk,
+                                        int D, const calibatt_window *window, float scale, const calibatt_strides *dout_strides,
+                                        const calibatt_strides *q_strides, const calibatt_strides *kv_strides,
+                                        const calibatt_strides *out_strides, const calibatt_strides *dq_strides,
+                                        const calibatt_strides *dkv_strides, int dtype, void *workspace,
+                                        int64_t workspace_bytes, void *stream) {
+  if (!dout || !q || !k || !v || !out || !lse || !dq || !dk || !dv || !window || !workspace) return CALIBATT_ERR_NULL;
+  if (int st = window_check(B, Hq, Hkv, Nq, Nk, D, *window)) return st;
+  if (dtype != CALIBATT_BF16 && dtype != CALIBATT_F16) return CALIBATT_ERR_UNSUPPORTED;
+  if (!(scale - scale == 0.f) || dk == dv) return CALIBATT_ERR_SHAPE;
+  // the second kernel reads what the first has read, so no result may lie where an input does
+  const void *const inputs[] = {dout, q, k, v, out, lse};
+  for (const void *x : inputs)
+    if (x == dq || x == dk || x == dv || x == workspace) return CALIBATT_ERR_SHAPE;
+  if (dq == dk || dq == dv) return CALIBATT_ERR_SHAPE;
+  WindowDims p;
+  window_dims(B, Hq, Hkv, Nq, Nk, *window, scale, p);
+  if (!window_strides(dout_strides, B, Hq, Nq, D, p.dout) || !window_strides(q_strides, B, Hq, Nq, D, p.q) ||
+      !window_strides(kv_strides, B, Hkv, Nk, D, p.kv) || !window_strides(out_strides, B, Hq, Nq, D, p.out) ||
+      !window_strides(dq_strides, B, Hq, Nq, D, p.dq) || !window_strides(dkv_strides, B, Hkv, Nk, D, p.dkv))
+    return CALIBATT_ERR_SHAPE;
+  uintptr_t at = 0;
+  for (const void *x : {dout, q, k, v, out, (const void *)dq, (const void *)dk, (const void *)dv, (const void *)workspace}) at |= (uintptr_t)x;
+  if ((at & 15) || ((uintptr_t)lse & 3)) return CALIBATT_ERR_SHAPE;
+  const GradPlan g = grad_plan(B, Hq, Hkv, Nq, Nk, D, *window);
+  if (workspace_bytes < g.bytes) return CALIBATT_ERR_BUFFER_TOO_SMALL;
+  p.bwd_parts = g.parts;
+  p.bwd_sink_parts = g.sink_parts;
+  p.n_sink_blocks = g.sink_blocks;
+  p.part_dkv = (float *)workspace + ((int64_t)B * Hq * Nq + 3) / 4 * 4;
+  const GradTensors t = {(const uint16_t *)dout, (const uint16_t *)q, (const uint16_t *)k, (const uint16_t *)v,
+                         (const uint16_t *)out, lse, (uint16_t *)dq, (uint16_t *)dk, (uint16_t *)dv, (float *)workspace};
+  hipStream_t s = (hipStream_t)stream;
+  if (D == 128) return dtype == CALIBATT_BF16 ? launch_backward<128, Bf16>(t, p, g, s) : launch_backward<128, F16>(t, p, g, s);
+  return dtype == CALIBATT_BF16 ? launch_backward<64, Bf16>(t, p, g, s) : launch_backward<64, F16>(t, p, g, s);
 }

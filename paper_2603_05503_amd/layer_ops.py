@@ -38,9 +38,12 @@ def declare(lib):
     lib.calibatt_layer_norm_bwd.argtypes = [C.c_void_p] * 6 + [C.c_int64] * 3 + [C.c_int] + [C.c_void_p] * 3 + [
         C.c_float, C.c_int, C.c_int, C.c_int, C.c_void_p, C.c_int64, C.c_void_p]
     lib.calibatt_window_attn_workspace_bytes.restype = C.c_int
-    lib.calibatt_window_attn_workspace_bytes.argtypes = [C.c_int] * 6 + [C.c_void_p, i64p]
+    lib.calibatt_window_attn_workspace_bytes.argtypes = [C.c_int] * 6 + [C.c_void_p, i64p, i64p]
     lib.calibatt_window_attn_fwd.restype = C.c_int
     lib.calibatt_window_attn_fwd.argtypes = [C.c_void_p] * 5 + [C.c_int] * 6 + [C.c_void_p, C.c_float] + [C.c_void_p] * 3 + [
+        C.c_int, C.c_void_p, C.c_int64, C.c_void_p]
+    lib.calibatt_window_attn_bwd.restype = C.c_int
+    lib.calibatt_window_attn_bwd.argtypes = [C.c_void_p] * 9 + [C.c_int] * 6 + [C.c_void_p, C.c_float] + [C.c_void_p] * 6 + [
         C.c_int, C.c_void_p, C.c_int64, C.c_void_p]
 
 
@@ -301,7 +304,7 @@ class Window:
             if not -(2 ** 31) <= int(v) < 2 ** 31:
                 raise ValueError(f"{name} does not fit 32 bits")
         self.left, self.right, self.sinks, self.frame, self.offset = (int(v) for v in values.values())
-        self._bytes = {}  # sizes of a call -> workspace bytes of its forward
+        self._bytes = {}  # sizes of a call -> workspace bytes of its forward and of its gradients
 
     def _c(self, q_start, q_len, k_len, B, device):
         """The C struct of one call."""
@@ -316,17 +319,17 @@ class Window:
         return c
 
     def workspace_bytes(self, B: int, Hq: int, Hkv: int, Nq: int, Nk: int, D: int):
-        """calibatt_window_attn_workspace_bytes."""
+        """calibatt_window_attn_workspace_bytes: (forward, backward)."""
         key = (B, Hq, Hkv, Nq, Nk, D)
         n = self._bytes.get(key)
         if n is None:
-            c, got = _CWindow(self.left, self.right, self.sinks, self.frame, self.offset), C.c_int64(0)
-            st = _b.load_library().calibatt_window_attn_workspace_bytes(*key, C.addressof(c), C.byref(got))
+            c, fwd, bwd = _CWindow(self.left, self.right, self.sinks, self.frame, self.offset), C.c_int64(0), C.c_int64(0)
+            st = _b.load_library().calibatt_window_attn_workspace_bytes(*key, C.addressof(c), C.byref(fwd), C.byref(bwd))
             if st != 0:
                 raise _b.CalibattError(st, "calibatt_window_attn_workspace_bytes")
             if len(self._bytes) >= 256:
                 self._bytes.clear()
-            n = self._bytes[key] = got.value
+            n = self._bytes[key] = fwd.value, bwd.value
         return n
 
 
@@ -372,7 +375,7 @@ def window_attn_fwd(q, k, v, out, window: Window, scale: float, lse=None, q_star
     stream, other = _b._stream_of(stream, q.device)
     c = window._c(q_start, q_len, k_len, B, q.device)
     with _on(q.device):
-        nbytes, workspace = window.workspace_bytes(B, Hq, Hkv, Nq, Nk, D), None
+        nbytes, workspace = window.workspace_bytes(B, Hq, Hkv, Nq, Nk, D)[0], None
         if nbytes:
             try:
                 workspace = _b._empty(nbytes // 4, torch.float32, q.device, other)
@@ -386,3 +389,35 @@ def window_attn_fwd(q, k, v, out, window: Window, scale: float, lse=None, q_star
     if st != 0:
         raise _b.CalibattError(st, "calibatt_window_attn_fwd")
     return out
+
+
+def window_attn_bwd(dout, q, k, v, out, lse, window: Window, scale: float, dq=None, dk=None, dv=None, q_start=None, q_len=None,
+                    k_len=None, stream=None):
+    """calibatt_window_attn_bwd: (dq, dk, dv) for ``dout``, the gradient of what ``window_attn_fwd`` left in ``out`` for the same
+    arguments, and its ``lse``; new tensors unless given (dk and dv share their strides, no result may be an input)."""
+    import torch
+
+    lib = _b.load_library()
+    given = (("dout", dout), ("out", out)) if dq is None else (("dout", dout), ("out", out), ("dq", dq))
+    B, Hq, Nq, D, Hkv, Nk, dtype = _window_tensors(q, k, v, given)
+    _check_lse(lse, q)
+    if (dk is None) != (dv is None):
+        raise ValueError("dk and dv are given together")
+    stream, other = _b._stream_of(stream, q.device)
+    c = window._c(q_start, q_len, k_len, B, q.device)
+    with _on(q.device):
+        dq = _empty_like(q, other) if dq is None else dq
+        if dk is None:
+            dk, dv = _empty_like(k, other), _empty_like(k, other)
+        for t in (dk, dv):
+            if not (t.shape == k.shape and t.dtype == k.dtype and t.device == k.device and t.stride(3) == 1 and t.stride() == dk.stride()):
+                raise ValueError("dk and dv must have the shape, element type and device of k and share their strides")
+        nbytes = window.workspace_bytes(B, Hq, Hkv, Nq, Nk, D)[1]
+        workspace = _b._empty(nbytes // 4, torch.float32, q.device, other)
+        keep, at = _strides(dout, q, k, out, dq, dk)
+        st = lib.calibatt_window_attn_bwd(dout.data_ptr(), q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), lse.data_ptr(),
+                                          dq.data_ptr(), dk.data_ptr(), dv.data_ptr(), B, Hq, Hkv, Nq, Nk, D, C.addressof(c),
+                                          float(scale), *at, dtype, workspace.data_ptr(), nbytes, stream)
+    if st != 0:
+        raise _b.CalibattError(st, "calibatt_window_attn_bwd")
+    return dq, dk, dv

@@ -169,6 +169,149 @@ def test_window_large_logits_and_any_scale(lib, Nq, gain):
         assert (np.abs(f64(out) - want) <= half * 1.01 * (np.abs(want) + size) + 2.0 ** -10 * size + 1e-7).all()
 
 
+# ---- gradients ----------------------------------------------------------------------------------------------
+def grad_bounds(dout, q, k, v, see, scale, half):
+    """How far the gradients may be off.  P and dS are rounded to the element type (half a step of each, in every product),
+    delta is taken from the rounded output (half a step of sum |dO| |O|, times P), the results are rounded, and fp32 sums and
+    exponentials add 2^-14 of what they are sums of (2^8 roundings of 2^-24, logits of up to 2^6)."""
+    G = q.shape[1] // k.shape[1]
+    out, lse = layer.window_attention(q, k, v, see, scale)
+    dq, dk, dv = np.zeros(q.shape), np.zeros(k.shape), np.zeros(v.shape)
+    for b in range(q.shape[0]):
+        some = see[b].any(-1)
+        for h in range(q.shape[1]):
+            kk, vv = np.where(see[b].any(0)[:, None], k[b, h // G], 0.0), np.where(see[b].any(0)[:, None], v[b, h // G], 0.0)
+            qq, do = np.where(some[:, None], q[b, h], 0.0), np.where(some[:, None], dout[b, h], 0.0)
+            p = np.where(see[b], np.exp(np.where(see[b], qq @ kk.T * scale, 0.0) - np.where(some, lse[b, h], 0.0)[:, None]), 0.0)
+            delta = (do * out[b, h]).sum(-1, keepdims=True)
+            adelta = (np.abs(do) * np.abs(out[b, h])).sum(-1, keepdims=True)
+            ds = p * (half * np.abs(do @ vv.T - delta) + half * adelta + 2.0 ** -14 * (np.abs(do) @ np.abs(vv).T + adelta))
+            dq[b, h] = abs(scale) * ds @ np.abs(kk)
+            dk[b, h // G] += abs(scale) * ds.T @ np.abs(qq)
+            dv[b, h // G] += (half + 2.0 ** -14) * p.T @ np.abs(do)
+    return dq, dk, dv
+
+
+def check_grads(got, dout, q, k, v, see, scale, dtype):
+    torch = _torch()
+    half = 0.5 * torch.finfo(getattr(torch, dtype)).eps * 1.01
+    args = [f64(t) for t in (dout, q, k, v)]
+    want, bounds = layer.window_attention_grads(*args, see, scale), grad_bounds(*args, see, scale, half)
+    for name, g, w, bound in zip(("dq", "dk", "dv"), got, want, bounds):
+        g = f64(g)
+        assert np.isfinite(g).all(), name
+        off = np.abs(g - w) / (half * np.abs(w) + bound + 1e-7)
+        assert off.max() <= 1.0, f"{name}: worst {off.max():.2f} of what is allowed"
+        assert (g[bound == 0] == 0).all(), name  # nothing seen: exactly zero
+
+
+GRAD_CASES = CASES + [
+    # enough heads, or keys, for the wide blocks of either kernel
+    (1, 64, 64, 1030, 1030, 64, dict(left=100, right=0, sinks=5, frame=1)),
+    (1, 40, 40, 1801, 1801, 128, dict(left=1, right=0, sinks=300, frame=225)),
+    (2, 64, 32, 300, 530, 128, dict(left=-1, right=0, sinks=0, frame=1, offset=230)),
+    # a few sinks and many queries: their block's queries are cut
+    (1, 2, 1, 6000, 6000, 64, dict(left=64, right=0, sinks=4, frame=1)),
+]
+
+
+@pytest.mark.parametrize("B,Hq,Hkv,Nq,Nk,D,c", GRAD_CASES)
+@pytest.mark.parametrize("dtype,layout", [("bfloat16", "bnhd"), ("float16", "packed")])
+def test_window_gradients(lib, B, Hq, Hkv, Nq, Nk, D, c, dtype, layout):
+    torch = _torch()
+    print(f"grads {B} {Hq} {Hkv} {Nq} {Nk} {D} {c} {dtype} {layout}", flush=True)
+    rng = np.random.default_rng(Nq + 2 * Nk)
+    q, k, v, dout = (make(rng, s, dtype) for s in ((B, Hq, Nq, D), (B, Hkv, Nk, D), (B, Hkv, Nk, D), (B, Hq, Nq, D)))
+    scale, w = 1 / math.sqrt(D), lib.Window(**c)
+    qv, kv, vv, dv_ = (laid_out(t, layout) for t in (q, k, v, dout))
+    out, lse = laid_out(torch.empty_like(q), layout), torch.empty((B, Hq, Nq), device="cuda")
+    lib.window_attn_fwd(qv, kv, vv, out, w, scale, lse=lse)
+    got = lib.window_attn_bwd(dv_, qv, kv, vv, out, lse, w, scale)
+    if Hq * Nq * Nk < 3e7 or Hq == 2:
+        check_grads(got, dout, q, k, v, visible(c, B, Nq, Nk), scale, dtype)
+    else:  # the oracle on some of the heads
+        at = [0, Hq // 2, Hq - 1]
+        G = Hq // Hkv
+        for h in at:
+            hk = h // G
+            heads = slice(hk * G, hk * G + G)
+            check_grads((got[0][:, heads], got[1][:, hk:hk + 1], got[2][:, hk:hk + 1]), dout[:, heads], q[:, heads],
+                        k[:, hk:hk + 1], v[:, hk:hk + 1], visible(c, B, Nq, Nk), scale, dtype)
+    # given tensors of another layout, rows around them untouched; the same bits again
+    dq = laid_out(torch.full_like(q, 7.0), layout)
+    whole = torch.full((2, B, Nk + 2, Hkv, D), float("nan"), dtype=q.dtype, device="cuda")
+    dk, dv = (x[:, 1:Nk + 1].transpose(1, 2) for x in whole)
+    again = lib.window_attn_bwd(dout, q, k, v, out.contiguous(), lse, w, scale, dq=dq, dk=dk, dv=dv)
+    assert again[0] is dq and all(torch.equal(a, g) for a, g in zip(again, got))
+    assert torch.isnan(whole[:, :, 0]).all() and torch.isnan(whole[:, :, -1]).all()
+
+
+@pytest.mark.parametrize("B,Hq,Hkv,Nq,Nk,D,c,start,q_len,k_len", LENGTHS)
+@pytest.mark.parametrize("dtype", ["bfloat16", "float16"])
+def test_window_gradients_with_lengths(lib, B, Hq, Hkv, Nq, Nk, D, c, start, q_len, k_len, dtype):
+    """Padded batches: NaN in all rows that are not there or meet nothing, dout's among them."""
+    torch = _torch()
+    print(f"grads, lengths {B} {Nq} {Nk} {D} {c} {start} {q_len} {k_len} {dtype}", flush=True)
+    rng = np.random.default_rng(B + 3 * Nk)
+    q, k, v, dout = (make(rng, s, dtype) for s in ((B, Hq, Nq, D), (B, Hkv, Nk, D), (B, Hkv, Nk, D), (B, Hq, Nq, D)))
+    see = visible(c, B, Nq, Nk, np.clip(start, -(2 ** 30), 2 ** 30), q_len, k_len)
+    qn, kn, vn, dn = q.clone(), k.clone(), v.clone(), dout.clone()
+    for b in range(B):
+        qn[b, :, max(0, q_len[b]):] = float("nan")
+        dn[b, :, max(0, q_len[b]):] = float("nan")
+        unseen = torch.from_numpy(~see[b].any(0)).cuda()
+        past = torch.arange(Nk, device="cuda") >= k_len[b]
+        kn[b, :, unseen & past], vn[b, :, unseen & past] = float("nan"), float("nan")
+    at = dict(zip(("q_start", "q_len", "k_len"), (torch.tensor(np.array(x, dtype=np.int64).astype(np.int32), device="cuda") for x in (start, q_len, k_len))))
+    out, lse, w = torch.empty_like(q), torch.empty((B, Hq, Nq), device="cuda"), lib.Window(**c)
+    lib.window_attn_fwd(qn, kn, vn, out, w, 0.11, lse=lse, **at)
+    got = lib.window_attn_bwd(dn, qn, kn, vn, out, lse, w, 0.11, **at)
+    check_grads(got, dout, q, k, v, see, 0.11, dtype)
+
+
+def test_window_gradient_against_differences(lib):
+    """Directional differences of the fp64 forward at the library's inputs; and the oracle's gradients against them."""
+    rng = np.random.default_rng(9)
+    c, scale = dict(left=20, right=3, sinks=4, frame=1), 0.2
+    q, k, v, dout = (make(rng, s, "float16", 0.7) for s in ((1, 4, 90, 64), (1, 2, 90, 64), (1, 2, 90, 64), (1, 4, 90, 64)))
+    torch = _torch()
+    out, lse, w = torch.empty_like(q), torch.empty((1, 4, 90), device="cuda"), lib.Window(**c)
+    lib.window_attn_fwd(q, k, v, out, w, scale, lse=lse)
+    grads = lib.window_attn_bwd(dout, q, k, v, out, lse, w, scale)
+    see, args = visible(c, 1, 90, 90), [f64(t) for t in (q, k, v)]
+    exact = layer.window_attention_grads(f64(dout), *args, see, scale)
+    f = lambda a: (layer.window_attention(*a, see, scale)[0] * f64(dout)).sum()  # noqa: E731
+    for i in range(3):
+        u, step = rng.standard_normal(args[i].shape), 1e-5
+        up, dn = list(args), list(args)
+        up[i], dn[i] = up[i] + step * u, dn[i] - step * u
+        slope = (f(up) - f(dn)) / (2 * step)
+        assert abs(slope - (exact[i] * u).sum()) <= 1e-5 * max(1.0, abs(slope))
+        # 2^-11 of every term, as in grad_bounds, three roundings deep, over independent terms
+        assert abs(slope - (f64(grads[i]) * u).sum()) <= 4 * 2.0 ** -11 * np.sqrt((exact[i] ** 2 * u ** 2).sum()) * 8 + 1e-3
+
+
+def test_window_gradient_refusals(lib):
+    torch = _torch()
+    q, k = torch.zeros((1, 2, 64, 64), dtype=torch.bfloat16, device="cuda"), torch.zeros((1, 2, 96, 64), dtype=torch.bfloat16, device="cuda")
+    v, dout, out, lse, w = torch.zeros_like(k), torch.zeros_like(q), torch.zeros_like(q), torch.zeros((1, 2, 64), device="cuda"), lib.Window(4)
+    f = lib.window_attn_bwd
+    for call in (lambda: f(dout.half(), q, k, v, out, lse, w, 1.0), lambda: f(dout, q, k, v, out, lse.half(), w, 1.0),
+                 lambda: f(dout, q, k, v, out[:, :1], lse, w, 1.0), lambda: f(dout, q, k, v, out, lse, w, 1.0, dk=torch.zeros_like(k)),
+                 lambda: f(dout, q, k, v, out, lse, w, 1.0, dk=torch.zeros_like(q), dv=torch.zeros_like(q)),
+                 lambda: f(dout, q, k, v, out, lse, w, 1.0, dq=torch.zeros_like(k))):
+        with pytest.raises(ValueError):
+            call()
+    for call in (lambda: f(dout, q, k, v, out, lse, w, 1.0, dq=q), lambda: f(dout, q, k, v, out, lse, w, 1.0, dk=k, dv=torch.zeros_like(k)),
+                 lambda: f(dout, q, k, v, out, lse, w, math.nan), lambda: f(dout, q, k, v, out, lse, lib.Window(-5), 1.0)):
+        with pytest.raises(lib.CalibattError):
+            call()
+    dk = torch.zeros_like(k)
+    with pytest.raises(lib.CalibattError):
+        f(dout, q, k, v, out, lse, w, 1.0, dk=dk, dv=dk)
+    torch.cuda.synchronize()
+
+
 def test_window_refusals(lib):
     torch = _torch()
     q = torch.zeros((2, 4, 64, 64), dtype=torch.bfloat16, device="cuda")

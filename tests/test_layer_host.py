@@ -136,8 +136,8 @@ def _window(fn="bytes", B=2, Hq=4, Hkv=2, Nq=300, Nk=300, D=64, left=10, right=0
     w = _CWindow(left, right, sinks, frame, offset, q_start, None, None)
     lib = pkg.load_library()
     if fn == "bytes":
-        n = C.c_int64(-1)
-        st = lib.calibatt_window_attn_workspace_bytes(B, Hq, Hkv, Nq, Nk, D, C.addressof(w), C.byref(n))
+        n, back = C.c_int64(-1), C.c_int64(-1)
+        st = lib.calibatt_window_attn_workspace_bytes(B, Hq, Hkv, Nq, Nk, D, C.addressof(w), C.byref(n), C.byref(back))
         return st if st else n.value
     arrays = [None if s is None else (C.c_int64 * 3)(*s) for s in (sq, skv, so)]
     return lib.calibatt_window_attn_fwd(q, k, v, out, lse, B, Hq, Hkv, Nq, Nk, D, C.addressof(w), scale,
