@@ -6,11 +6,18 @@
 // one owns keys and goes over the queries that see them, of all query heads that share them (dK, dV).  Seven products
 // instead of five, but no sum goes through atomics: the same inputs give the same bits.
 //
-// Both are the same shape.  A wave owns NB blocks of 32 columns (its queries, or its keys) as second operands in
-// registers; tiles of 64 rows of two matrices (K and V, or Q and dO) pass through LDS, read row-wise for S^T and dP^T
-// (first operand: rows of the tile) and transposed for the products that add up, whose second operands are P and dS as
-// they lie in registers.  With NB = 2 a wave holds 512 registers and is alone on its SIMD, every LDS read feeds two MFMAs,
-// and it hides its vector work behind its own MFMAs: exponentials beside dP, dS beside the products with P.
+// Both are the same shape.  A wave owns 32 columns (its queries, or its keys) as second operands; tiles of 32 rows of two
+// matrices (K and V, or Q and dO) pass through LDS, read row-wise for S^T and dP^T (first operand: rows of the tile) and
+// transposed for the products that add up, whose second operands are P and dS as they lie in registers.  128 columns to a
+// workgroup, two workgroups per CU.
+//
+// A wave issues in order, an instruction every four cycles at best, and an MFMA that finds the matrix pipe busy holds up
+// what stands behind it.  So the work on 32 rows is written as a stream of GAPS: an MFMA, the read of the first operand of
+// two gaps later, a share of the vector work (exponentials beside dP and what follows it, dS behind them), a scheduling
+// barrier; the second wave of the SIMD fills what one leaves.  Us of dQ, and of dK and dV, for 16 380 tokens, 8 query heads
+// on 4 key heads, D = 128, nine frames of 780 and the first: scheduled by the compiler, 64 columns to a wave, one wave per
+// SIMD 930 and 2660 (it gathers reads and vector work and spills), the same in gaps 787 and 1253 (half its cycles waits),
+// this form @GAPS@.
 #pragma once
 #include "attn_kernel_window.h"
 
@@ -30,21 +37,62 @@ __device__ __forceinline__ int both_swz(int row) {
 template <typename T> struct GradScale { static constexpr float P_LOG2 = 0.f, DS = 1.f; };
 template <> struct GradScale<F16> { static constexpr float P_LOG2 = 15.f, DS = 16.f; };
 
-template <int D, int NB, typename T>
+// out (+)= a b.  Written out, because the compiler, given 512 registers, keeps every accumulator of an MFMA in AGPRs, from
+// where S and dP are copied element by element, and then moves the sums around them (700 copies per 128 MFMAs).  Here S
+// and dP are VGPRs (IN_V) and the sums AGPRs.  What the compiler does not know of an asm's MFMA is kept by hand: the
+// operands may just have been written by vector instructions (two wait states in front), and a result is read by others
+// only behind settle() (csrc/check_mfma_waits.py).
+// B_A: the second operand is in AGPRs as well.
+template <typename T, bool IN_V, bool FRESH, bool B_A = false>
+__device__ __forceinline__ void mfma_gap(f32x16 &out, const u32x4 a, const u32x4 b) {
+#define CALIBATT_GAP(op)                                                                                                  \
+  if constexpr (FRESH && B_A) asm volatile("s_nop 1\n\t" op " %0, %1, %2, 0" : "=&v"(out) : "v"(a), "a"(b));              \
+  else if constexpr (FRESH) asm volatile("s_nop 1\n\t" op " %0, %1, %2, 0" : "=&v"(out) : "v"(a), "v"(b));                \
+  else if constexpr (IN_V && B_A) asm volatile("s_nop 1\n\t" op " %0, %1, %2, %0" : "+v"(out) : "v"(a), "a"(b));          \
+  else if constexpr (IN_V) asm volatile("s_nop 1\n\t" op " %0, %1, %2, %0" : "+v"(out) : "v"(a), "v"(b));                 \
+  else asm volatile("s_nop 1\n\t" op " %0, %1, %2, %0" : "+a"(out) : "v"(a), "v"(b));
+  if constexpr (std::is_same<T, Bf16>::value) {
+    CALIBATT_GAP("v_mfma_f32_32x32x16_bf16")
+  } else {
+    CALIBATT_GAP("v_mfma_f32_32x32x16_f16")
+  }
+#undef CALIBATT_GAP
+}
+// Everything read behind this sees the results of the MFMAs in front of it.
+template <bool IN_V>
+__device__ __forceinline__ void settle(f32x16 &x) {
+  if constexpr (IN_V) asm volatile("s_nop 15" : "+v"(x));
+  else asm volatile("s_nop 15" : "+a"(x));
+}
+
+template <int D, typename T>
 struct GradTile {
-  static constexpr int NT = 256, ROWS = 64, ROWB = D * 2, CH = D / 8, DS = D / 16, DB = D / 32;
-  static constexpr int TILE = ROWS * ROWB;           // bytes of one matrix's tile
-  static constexpr int RPI = NT / CH, ITERS = ROWS / RPI;
+  static constexpr int NT = 256, COLS = 32, BLOCK = 4 * COLS;    // columns of a wave, of the workgroup
+  static constexpr int ROWS = 32, ROWB = D * 2, CH = D / 8, DS = D / 16, DB = D / 32;
+  static constexpr int TILE = ROWS * ROWB, PAIR = 2 * TILE;      // bytes of one matrix's tile, of both
+  static constexpr int RPI = NT / CH, ITERS = ROWS / RPI, LOADS = 2 * ITERS;  // load instructions of a wave for a pair
   static_assert(RPI % 16 == 0, "the swizzle of an instruction's rows is the same for every one");
-  static constexpr int LDS_BYTES = 4 * TILE;         // two buffers of two matrices
-  static constexpr int COLS = NB * 32;               // columns of a wave
-  static constexpr float P_UNIT = GradScale<T>::P_LOG2 == 0.f ? 1.f : 1.f / 32768.f;   // what P_LOG2 stands for
-  static constexpr float DS_OF_P = GradScale<T>::DS * P_UNIT;                          // factor of dP - delta beside P as kept
+  static constexpr float P_UNIT = GradScale<T>::P_LOG2 == 0.f ? 1.f : 1.f / 32768.f;  // what P_LOG2 stands for
+  static constexpr float DS_OF_P = GradScale<T>::DS * P_UNIT;                         // factor of dP - delta beside P as kept
+
+  // A phase (S, dP, or one of the products that add up) has PH gaps.  The UNITS of vector work of 32 rows, pairs of a lane's
+  // values, by their gap behind the start of dP: exponentials over 22/16 of a phase, then each pair's dS, in dK and dV's
+  // kernel over 18/16, in dQ's over the 10/16 that are left before S of the next rows.  In the former the first halves are
+  // needed half a phase before the second ones: probabilities from gap PH on (dV), dS from gap 2 PH on (dK).
+  static constexpr int PH = DS, UNITS = 8, EXP_GAPS = 22 * PH / 16;
+  static_assert(DS == 2 * DB, "phases of the same length");
+  static constexpr int exp_gap(int u) { return u * EXP_GAPS / UNITS; }
+  static constexpr int ds_gap(int u) { return EXP_GAPS + u * (18 * PH / 16) / UNITS; }
+  static constexpr int dq_ds_gap(int u) { return EXP_GAPS + u * (2 * PH - EXP_GAPS) / UNITS; }
+  static_assert(exp_gap(UNITS / 2 - 1) < PH && exp_gap(UNITS - 1) < PH + PH / 2, "probabilities are there before dV");
+  static_assert(EXP_GAPS >= PH && ds_gap(UNITS / 2 - 1) < 2 * PH && ds_gap(UNITS - 1) < 2 * PH + PH / 2, "dS is there before dK");
+  static_assert(dq_ds_gap(UNITS - 1) < 2 * PH, "S of the next rows takes the place of this one's");
 
   int tid, lane, wave, l32, g;
-  uint32_t row_addr;     // row-wise reads: chunk column s at row_addr ^ (s << 5), 32 rows on at + 32 * ROWB
+  uint32_t row_addr;     // row-wise reads: chunk column s at row_addr ^ (s << 5)
   uint32_t col_addr[2];  // transposed reads: d block db at col_addr[t] ^ (db << 6), slab j at + 16 j * ROWB
-  uint32_t lds_wave;
+  uint32_t second_addr;  // operands of columns that stay in LDS: chunk column s at second_addr ^ (s << 5)
+  uint32_t lds_base, lds_wave;
 
   __device__ __forceinline__ explicit GradTile(char *lds) {
     tid = threadIdx.x;
@@ -52,10 +100,11 @@ struct GradTile {
     wave = tid >> 6;
     l32 = lane & 31;
     g = lane >> 5;
-    const uint32_t base = (uint32_t)(uintptr_t)(LDS_PTR(char))lds;
-    lds_wave = __builtin_amdgcn_readfirstlane(base + wave * 1024);
+    lds_base = (uint32_t)(uintptr_t)(LDS_PTR(char))lds;  // a multiple of 1024
+    lds_wave = __builtin_amdgcn_readfirstlane(lds_base + wave * 1024);
     const int row = (l32 & 0x13) | ((l32 & 4) << 1) | ((l32 & 8) >> 1);  // so that a lane's eight values are of consecutive rows
     row_addr = row * ROWB + ((g ^ both_swz<D>(row)) << 4);
+    second_addr = l32 * ROWB + ((g ^ both_swz<D>(l32)) << 4);
     const int L16 = lane & 15, blk = lane >> 4;
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
@@ -63,7 +112,7 @@ struct GradTile {
       col_addr[t] = r * ROWB + (((2 * (blk & 1) + ((L16 & 3) >> 1)) ^ both_swz<D>(r)) << 4) + (L16 & 1) * 8;
     }
   }
-  // rows [row0, row0 + 64) of a matrix into the tile at LDS byte `at`
+  // rows [row0, row0 + 32) of a matrix into the tile at LDS byte `at`
   __device__ __forceinline__ void issue(const u32x4 rsrc, int row0, uint32_t at, uint32_t row_bytes) const {
     const int row = tid / CH, c = (tid % CH) ^ both_swz<D>(row);
     const uint32_t voff = row * row_bytes + c * 16;
@@ -76,33 +125,34 @@ struct GradTile {
 #pragma unroll
     for (int s = 0; s < DS; ++s) x[s] = *reinterpret_cast<const u32x4 *>(row + 16 * s + 8 * g);
   }
-  // out[c] = (rows [32 half, 32 half + 32) of the tile) . columns
-  __device__ __forceinline__ void products(const char *tile, int half, const u32x4 (&x)[NB][DS], f32x16 (&out)[NB]) const {
-#pragma unroll
-    for (int c = 0; c < NB; ++c)
-#pragma unroll
-      for (int v = 0; v < 16; ++v) out[c][v] = 0.f;
+  // waits for the loads of operands here, and not inside the loop, where tiles are on their way as well
+  template <bool IN_A = false>
+  static __device__ __forceinline__ void arrive(u32x4 (&x)[DS]) {
 #pragma unroll
     for (int s = 0; s < DS; ++s) {
-      const u32x4 a = *reinterpret_cast<const u32x4 *>(tile + half * 32 * ROWB + (row_addr ^ (s << 5)));
-#pragma unroll
-      for (int c = 0; c < NB; ++c) out[c] = T::mfma(a, x[c][s], out[c]);
+      if constexpr (IN_A) asm volatile("" : "+a"(x[s]));
+      else asm volatile("" : "+v"(x[s]));
     }
   }
-  // sum[c][db] += (rows [32 half, + 32) of the tile)^T . weights, weights as packed pairs of the rows' values
-  __device__ __forceinline__ void add(const char *tile, int half, const uint32_t (&w)[NB][8], f32x16 (&sum)[NB][DB]) const {
-#pragma unroll
-    for (int j = 0; j < 2; ++j)
-#pragma unroll
-      for (int db = 0; db < DB; ++db) {
-        const char *const at = tile + (half * 32 + 16 * j) * ROWB;
-        const u32x2 lo = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4bf16((LDS_PTR(bf16x4))(at + (col_addr[0] ^ (db << 6)))));
-        const u32x2 hi = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4bf16((LDS_PTR(bf16x4))(at + (col_addr[1] ^ (db << 6)))));
-        const u32x4 a = {lo[0], lo[1], hi[0], hi[1]};
-#pragma unroll
-        for (int c = 0; c < NB; ++c) sum[c][db] = T::mfma(a, u32x4{w[c][4 * j], w[c][4 * j + 1], w[c][4 * j + 2], w[c][4 * j + 3]}, sum[c][db]);
-      }
+  // First operands: slab s of a tile's rows, and their transpose's 16-row slab j and 32-wide d block db.  `at`: LDS address
+  // of this lane's piece of a pair of tiles (see Places), `off`: of the tile in the pair.
+  static __device__ __forceinline__ u32x4 rows_of(uint32_t at, int off, int s) {
+    return *(LDS_PTR(const u32x4))(uintptr_t)((at ^ (s << 5)) + off);
   }
+  static __device__ __forceinline__ u32x4 cols_of(const uint32_t (&at)[2], int off, int j, int db) {
+    off += 16 * j * ROWB;
+    const u32x2 lo = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4bf16((LDS_PTR(bf16x4))(uintptr_t)((at[0] ^ (db << 6)) + off)));
+    const u32x2 hi = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4bf16((LDS_PTR(bf16x4))(uintptr_t)((at[1] ^ (db << 6)) + off)));
+    return u32x4{lo[0], lo[1], hi[0], hi[1]};
+  }
+  // Addresses of a pair of tiles.  They pass through an empty asm, so that the many that are derived from them are formed
+  // where they are used (one instruction) instead of kept in registers.
+  struct Places {
+    uint32_t rows, cols[2];
+    __device__ __forceinline__ Places(const GradTile &t, uint32_t pair) : rows(t.row_addr + pair), cols{t.col_addr[0] + pair, t.col_addr[1] + pair} {
+      asm volatile("" : "+v"(rows), "+v"(cols[0]), "+v"(cols[1]));
+    }
+  };
   // a column's D sums times f, rounded, to its row in memory; zeros for a row that is not `there`
   static __device__ __forceinline__ void store(const f32x16 (&sum)[DB], float f, bool there, uint16_t *row, int g) {
 #pragma unroll
@@ -116,14 +166,18 @@ struct GradTile {
 };
 
 // ---- dQ -----------------------------------------------------------------------------------------------------
-template <int D, int NB, typename T>
-__global__ __launch_bounds__(256, NB == 2 ? 1 : 2) void window_attn_dq_kernel(
+// The tiles lie in four buffers: in its turn tile t is read for dP, t - 1 for dQ and t + 1 for S, while t + 2 is on its way.
+template <int D, typename T>
+constexpr int dq_lds_bytes() { return 4 * GradTile<D, T>::PAIR; }
+
+template <int D, typename T>
+__global__ __launch_bounds__(256, 2) void window_attn_dq_kernel(
     const uint16_t *__restrict__ gdo, const uint16_t *__restrict__ gq, const uint16_t *__restrict__ gk,
     const uint16_t *__restrict__ gv, const uint16_t *__restrict__ gout, const float *__restrict__ lse,
     uint16_t *__restrict__ gdq, float *__restrict__ delta, const WindowDims p) {
-  using Tile = GradTile<D, NB, T>;
-  using Tiles = WindowTiles<64>;
-  constexpr int BQ = 4 * Tile::COLS, DS = Tile::DS, DB = Tile::DB;
+  using Tile = GradTile<D, T>;
+  using Tiles = WindowTiles<Tile::ROWS>;
+  constexpr int BQ = Tile::BLOCK, DS = Tile::DS, DB = Tile::DB;
   extern __shared__ __attribute__((aligned(1024))) char lds[];
   const int nbq = (p.Nq + BQ - 1) / BQ;
   const int unit = window_unit(p.B * p.Hq * nbq);
@@ -131,19 +185,13 @@ __global__ __launch_bounds__(256, NB == 2 ? 1 : 2) void window_attn_dq_kernel(
   const int bh = unit / nbq, r = nbq - 1 - (unit - bh * nbq), b = bh / p.Hq, h = bh - b * p.Hq;
   const WindowEntry e(p, b);
   const Tile w(lds);
-  const int i0 = r * BQ, i1 = min(i0 + BQ, e.q_len);
+  const int i0 = r * BQ, i1 = min(i0 + BQ, e.q_len), col = i0 + w.wave * Tile::COLS + w.l32;
   const size_t row0 = (size_t)bh * p.Nq;
-  uint16_t *const dq_head = gdq + (size_t)b * p.dq.b + (size_t)h * p.dq.h;
-  f32x16 dq[NB][DB];
-  int col[NB];
+  f32x16 dq[DB];
 #pragma unroll
-  for (int c = 0; c < NB; ++c) {
-    col[c] = i0 + w.wave * Tile::COLS + 32 * c + w.l32;
+  for (int db = 0; db < DB; ++db)
 #pragma unroll
-    for (int db = 0; db < DB; ++db)
-#pragma unroll
-      for (int v = 0; v < 16; ++v) dq[c][db][v] = 0.f;
-  }
+    for (int v = 0; v < 16; ++v) dq[db][v] = 0.f;
   if (i0 < i1) {
     const Tiles tiles(p, e, i0, i1);
     const size_t kv_head = (size_t)b * p.kv.b + (size_t)(h / (p.Hq / p.Hkv)) * p.kv.h;
@@ -153,83 +201,120 @@ __global__ __launch_bounds__(256, NB == 2 ? 1 : 2) void window_attn_dq_kernel(
       const int end = t < tiles.n ? tiles.end(t) : 0;
       Kres[2] = Vres[2] = __builtin_amdgcn_readfirstlane(end > 0 ? (uint32_t)(end - 1) * row_bytes + Tile::ROWB : 0u);
       const int first = __builtin_amdgcn_readfirstlane(t < tiles.n ? tiles.row(t) : 0);
-      const uint32_t at = (t & 1) * 2 * Tile::TILE;
+      const uint32_t at = (uint32_t)(t & 3) * Tile::PAIR;
       w.issue(Kres, first, at, row_bytes);
       w.issue(Vres, first, at + Tile::TILE, row_bytes);
     };
     issue(0);
-    u32x4 q[NB][DS], dout[NB][DS];
-    float lse2[NB], dl[NB];
-    int lo[NB], hi[NB];
-#pragma unroll
-    for (int c = 0; c < NB; ++c) {
-      const int row = min(col[c], i1 - 1);  // columns behind the last query: its values, not stored
-      e.interval(p, row, lo[c], hi[c]);
-      w.operand(gq + (size_t)b * p.q.b + (size_t)h * p.q.h + (size_t)row * p.q.n, q[c]);
-      w.operand(gdo + (size_t)b * p.dout.b + (size_t)h * p.dout.h + (size_t)row * p.dout.n, dout[c]);
+    u32x4 q[DS], dout[DS];
+    int lo, hi;
+    const int row = min(col, i1 - 1);  // columns behind the last query: its values, not stored
+    e.interval(p, row, lo, hi);
+    w.operand(gq + (size_t)b * p.q.b + (size_t)h * p.q.h + (size_t)row * p.q.n, q);
+    w.operand(gdo + (size_t)b * p.dout.b + (size_t)h * p.dout.h + (size_t)row * p.dout.n, dout);
+    const float z = lse[row0 + row];
+    // a query that sees nothing: exponents of -inf
+    const float lse2 = z == -INFINITY ? INFINITY : z * 1.4426950408889634f - GradScale<T>::P_LOG2;
+    float dl = 0.f;
+    {
       u32x4 o[DS];
       w.operand(gout + (size_t)b * p.out.b + (size_t)h * p.out.h + (size_t)row * p.out.n, o);
-      const float z = lse[row0 + row];
-      float sum = 0.f;
 #pragma unroll
       for (int s = 0; s < DS; ++s)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          const uint32_t x = dout[c][s][i], y = o[s][i];
+          const uint32_t x = dout[s][i], y = o[s][i];
           float x2[2], y2[2];
           T::unpack(x, x2);
           T::unpack(y, y2);
-          sum = __builtin_fmaf(x2[0], y2[0], sum);
-          sum = __builtin_fmaf(x2[1], y2[1], sum);
+          dl = __builtin_fmaf(x2[0], y2[0], dl);
+          dl = __builtin_fmaf(x2[1], y2[1], dl);
         }
-      dl[c] = sum_with_other_half(sum);
-      // a query that sees nothing: exponents of -inf
-      lse2[c] = z == -INFINITY ? INFINITY : z * 1.4426950408889634f - GradScale<T>::P_LOG2;
-      if (w.g == 0 && col[c] < i1) delta[row0 + col[c]] = dl[c];
-      dl[c] *= Tile::DS_OF_P;
+      dl = sum_with_other_half(dl);
+      if (w.g == 0 && col < i1) delta[row0 + col] = dl;
+      dl *= Tile::DS_OF_P;
     }
-    const float sc = p.scale_log2e;
+    // dO in AGPRs, beside dQ: the compiler halves the registers, and the VGPRs are for the rest
+    Tile::arrive(q);
+    Tile::template arrive<true>(dout);
+    // the logit of an unseen key: -inf behind its product with the scale, which is not zero
+    const float sc = p.scale_log2e == 0.f ? 1e-30f : p.scale_log2e, unseen = sc < 0.f ? INFINITY : -INFINITY;
+    f32x16 s, dp;
+    u32x4 ds[2], ds_before[2], a[3];
+    ds_before[0] = ds_before[1] = u32x4{0, 0, 0, 0};
+    issue(1);
+    asm volatile("s_waitcnt vmcnt(%0)" : : "n"(Tile::LOADS) : "memory");
+    __syncthreads();
+    auto place_of = [&](int t) { return typename Tile::Places(w, w.lds_base + (uint32_t)(t & 3) * Tile::PAIR); };
+    typename Tile::Places before = place_of(0);  // (dS before tile 0 is zero)
+    static_unroll<DS>([&](auto k) {
+      a[0] = Tile::rows_of(before.rows, 0, k);
+      mfma_gap<T, true, k == 0>(s, a[0], q[k]);
+    });
+    a[0] = Tile::rows_of(before.rows, Tile::TILE, 0);
+    a[1] = Tile::rows_of(before.rows, Tile::TILE, 1);
     for (int t = 0; t < tiles.n; ++t) {
-      asm volatile("s_waitcnt vmcnt(0)" : : : "memory");
-      __syncthreads();  // tile t is there, and every wave is done with tile t - 1
-      issue(t + 1);
-      const char *const kt = lds + (t & 1) * 2 * Tile::TILE, *const vt = kt + Tile::TILE;
-      const bool whole = tiles.whole(t);
+      // dP, dQ of tile t - 1, S of tile t + 1; exponentials and dS beside the first two
+      const typename Tile::Places at = place_of(t), next = place_of(t + 1);
+      constexpr int N = 3 * DS;
+      static_assert(N % 3 == 0, "the operands' places go on with the next tile");
+      auto fetch = [&](auto q) {  // the operand of gap q (behind the last one: of tile t + 1)
+        constexpr int i = q;
+        if constexpr (i < DS) a[i % 3] = Tile::rows_of(at.rows, Tile::TILE, i);
+        else if constexpr (i < 2 * DS) a[i % 3] = Tile::cols_of(before.cols, 0, (i - DS) / DB, (i - DS) % DB);
+        else if constexpr (i < N) a[i % 3] = Tile::rows_of(next.rows, 0, i - 2 * DS);
+        else a[i % 3] = Tile::rows_of(next.rows, Tile::TILE, i - N);
+      };
+      static_unroll<N>([&](auto gap) {
+        constexpr int g = gap;
+        if constexpr (g == 2 * DS - 2) {
+          asm volatile("s_waitcnt vmcnt(0)" : : : "memory");
+          __syncthreads();  // tile t + 1 is there, and every wave is done with tile t - 2, whose place t + 2 takes
+          issue(t + 2);
+        }
+        fetch(std::integral_constant<int, g + 2>{});
+        if constexpr (g < DS) mfma_gap<T, true, g == 0, true>(dp, a[g % 3], dout[g]);
+        else if constexpr (g < 2 * DS) mfma_gap<T, false, false>(dq[(g - DS) % DB], a[g % 3], ds_before[(g - DS) / DB]);
+        else mfma_gap<T, true, g == 2 * DS>(s, a[g % 3], q[g - 2 * DS]);
+        if constexpr (g == 0) {
+          settle<true>(s);
+          if (!tiles.whole(t)) {  // the keys that a query does not see: a probability of 2^-inf
+            int from, end;
+            tile_interval(tiles, t, lo, hi, from, end);
+            const uint32_t span = (uint32_t)max(end - from, 0);
+            from = tiles.row(t) + 8 * w.g - from;
 #pragma unroll
-      for (int half = 0; half < 2; ++half) {
-        f32x16 s[NB], dp[NB];
-        uint32_t ds[NB][8];
-        w.products(kt, half, q, s);
-        w.products(vt, half, dout, dp);
-#pragma unroll
-        for (int c = 0; c < NB; ++c) {
-          if (!whole) {
-            int a, z;
-            tile_interval(tiles, t, lo[c], hi[c], a, z);
-            const int first = tiles.row(t) + 32 * half + 8 * w.g - a;
-            const uint32_t span = (uint32_t)max(z - a, 0);
-#pragma unroll
-            for (int v = 0; v < 16; ++v) s[c][v] = (uint32_t)(first + 16 * (v >> 3) + (v & 7)) < span ? s[c][v] * sc : -INFINITY;
-          } else {
-#pragma unroll
-            for (int v = 0; v < 16; ++v) s[c][v] *= sc;
-          }
-#pragma unroll
-          for (int v = 0; v < 16; v += 2) {
-            const float p0 = __builtin_amdgcn_exp2f(s[c][v] - lse2[c]), p1 = __builtin_amdgcn_exp2f(s[c][v + 1] - lse2[c]);
-            ds[c][v >> 1] = T::pack(p0 * __builtin_fmaf(dp[c][v], Tile::DS_OF_P, -dl[c]),
-                                    p1 * __builtin_fmaf(dp[c][v + 1], Tile::DS_OF_P, -dl[c]));
+            for (int v = 0; v < 16; ++v) s[v] = (uint32_t)(from + 16 * (v >> 3) + (v & 7)) < span ? s[v] : unseen;
           }
         }
-        w.add(kt, half, ds, dq);
-      }
+        if constexpr (g == Tile::EXP_GAPS) settle<true>(dp);
+        static_unroll<Tile::UNITS>([&](auto u) {
+          constexpr int v = 2 * u;
+          if constexpr (Tile::exp_gap(u) == g) {
+            s[v] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[v], sc, -lse2));
+            s[v + 1] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[v + 1], sc, -lse2));
+          }
+          if constexpr (Tile::dq_ds_gap(u) == g)
+            ds[v >> 3][(v >> 1) & 3] = T::pack(s[v] * __builtin_fmaf(dp[v], Tile::DS_OF_P, -dl), s[v + 1] * __builtin_fmaf(dp[v + 1], Tile::DS_OF_P, -dl));
+        });
+        __builtin_amdgcn_sched_barrier(0);
+      });
+      before = at;
+      ds_before[0] = ds[0];
+      ds_before[1] = ds[1];
     }
+    settle<true>(s);  // nothing reads the last S, but its registers are written again
+    if (tiles.n > 0)
+      static_unroll<DS>([&](auto k) {
+        a[0] = Tile::cols_of(before.cols, 0, k / DB, k % DB);
+        mfma_gap<T, false, false>(dq[k % DB], a[0], ds_before[k / DB]);
+      });
     asm volatile("s_waitcnt vmcnt(0)" : : : "memory");
-  }
-  const float f = p.scale / GradScale<T>::DS;
 #pragma unroll
-  for (int c = 0; c < NB; ++c)
-    if (col[c] < p.Nq) Tile::store(dq[c], f, col[c] < i1, dq_head + (size_t)col[c] * p.dq.n, w.g);
+    for (int db = 0; db < DB; ++db) settle<false>(dq[db]);
+  }
+  if (col < p.Nq)
+    Tile::store(dq, p.scale / GradScale<T>::DS, col < i1, gdq + (size_t)b * p.dq.b + (size_t)h * p.dq.h + (size_t)col * p.dq.n, w.g);
 }
 
 // ---- dK, dV -------------------------------------------------------------------------------------------------
@@ -263,15 +348,27 @@ __device__ __forceinline__ int grad_units(const WindowDims &p, int n_blocks) {
   return p.n_sink_blocks * p.bwd_sink_parts + (n_blocks - p.n_sink_blocks) * p.bwd_parts;
 }
 
-template <int D, int NB, typename T>
-__global__ __launch_bounds__(256, NB == 2 ? 1 : 2) void window_attn_dkv_kernel(
+// At D = 128 the sums, K and V of 32 columns are 192 of a wave's 256 registers, and what is left spills; so the operands of
+// K stay in LDS there, where reading them takes the reads of 32 rows from 32 to 40 KB a wave.
+template <int D>
+constexpr bool DKV_K_IN_LDS = D == 128;
+template <int D, typename T>
+constexpr int dkv_lds_bytes() {
+  using Tile = GradTile<D, T>;
+  return 2 * Tile::PAIR + 1024 + (DKV_K_IN_LDS<D> ? Tile::BLOCK * Tile::ROWB : 0);
+}
+
+template <int D, typename T>
+__global__ __launch_bounds__(256, 2) void window_attn_dkv_kernel(
     const uint16_t *__restrict__ gdo, const uint16_t *__restrict__ gq, const uint16_t *__restrict__ gk,
     const uint16_t *__restrict__ gv, const float *__restrict__ lse, const float *__restrict__ delta,
     uint16_t *__restrict__ gdk, uint16_t *__restrict__ gdv, const WindowDims p) {
-  using Tile = GradTile<D, NB, T>;
-  constexpr int BKV = 4 * Tile::COLS, DS = Tile::DS, DB = Tile::DB;
+  using Tile = GradTile<D, T>;
+  constexpr int BKV = Tile::BLOCK, DS = Tile::DS, DB = Tile::DB, ROWS = Tile::ROWS;
+  constexpr bool K_LDS = DKV_K_IN_LDS<D>;
   extern __shared__ __attribute__((aligned(1024))) char lds[];
-  float *const stats = reinterpret_cast<float *>(lds + Tile::LDS_BYTES);  // [2 buffers][lse2 of 64 rows, delta of 64 rows]
+  // [2 buffers][Q, dO tiles], [2 buffers][lse2 of 32 rows, delta of 32 rows], K of the block
+  float *const stats = reinterpret_cast<float *>(lds + 2 * Tile::PAIR);
   const int nkb = (p.Nk + BKV - 1) / BKV, per_head = grad_units(p, nkb);
   const int unit = window_unit(p.B * p.Hkv * per_head);
   if (unit < 0) return;
@@ -291,38 +388,35 @@ __global__ __launch_bounds__(256, NB == 2 ? 1 : 2) void window_attn_dkv_kernel(
   }
   const WindowEntry e(p, b);
   const Tile w(lds);
-  const int j0 = block * BKV, j1 = min(j0 + BKV, e.k_len), G = p.Hq / p.Hkv;
-  f32x16 dk[NB][DB], dv[NB][DB];
-  int col[NB];
+  const int j0 = block * BKV, j1 = min(j0 + BKV, e.k_len), G = p.Hq / p.Hkv, col = j0 + w.wave * Tile::COLS + w.l32;
+  f32x16 dk[DB], dv[DB];
 #pragma unroll
-  for (int c = 0; c < NB; ++c) {
-    col[c] = j0 + w.wave * Tile::COLS + 32 * c + w.l32;
+  for (int db = 0; db < DB; ++db)
 #pragma unroll
-    for (int db = 0; db < DB; ++db)
-#pragma unroll
-      for (int v = 0; v < 16; ++v) dk[c][db][v] = dv[c][db][v] = 0.f;
-  }
+    for (int v = 0; v < 16; ++v) dk[db][v] = dv[db][v] = 0.f;
   if (j0 < j1) {
     const WindowQueries seen(p, e, j0, j1);
-    const int n_tiles = max(0, seen.end - seen.begin + 63) / 64;
+    const int n_tiles = max(0, seen.end - seen.begin + ROWS - 1) / ROWS;
     const int u0 = (int)((long long)G * n_tiles * part / parts), u1 = (int)((long long)G * n_tiles * (part + 1) / parts);
     if (u0 < u1) {
       const uint32_t q_bytes = (uint32_t)p.q.n * 2, do_bytes = (uint32_t)p.dout.n * 2;
       const uint32_t q_limit = (uint32_t)(seen.end - 1) * q_bytes + Tile::ROWB, do_limit = (uint32_t)(seen.end - 1) * do_bytes + Tile::ROWB;
-      float stat = 0.f;  // of row tid & 63 of the tile that is on its way: threads 0..63 lse, 64..127 delta
+      // the tile that is asked for next: its head and first row; and of wave 0's lanes the lse or delta of a row of it
+      int next_h = __builtin_amdgcn_readfirstlane(hk * G + u0 / n_tiles), next_row = __builtin_amdgcn_readfirstlane(seen.begin + ROWS * (u0 % n_tiles));
+      float stat = 0.f;
       auto issue = [&](int u) {
-        const int h = hk * G + u / n_tiles, first = seen.begin + 64 * (u % n_tiles), at = (u & 1) * 2 * Tile::TILE;
         const bool there = u < u1;
-        const u32x4 Qres = head_rsrc(gq + (size_t)b * p.q.b + (size_t)(there ? h : 0) * p.q.h, there ? q_limit : 0u);
-        const u32x4 Dres = head_rsrc(gdo + (size_t)b * p.dout.b + (size_t)(there ? h : 0) * p.dout.h, there ? do_limit : 0u);
-        w.issue(Qres, __builtin_amdgcn_readfirstlane(first), at, q_bytes);
-        w.issue(Dres, __builtin_amdgcn_readfirstlane(first), at + Tile::TILE, do_bytes);
-        if (w.wave < 2) {
-          const int row = first + w.lane;
-          stat = w.wave == 0 ? INFINITY : 0.f;  // a row that is not there, or sees nothing: exponents of -inf
+        const u32x4 Qres = head_rsrc(gq + (size_t)b * p.q.b + (size_t)(there ? next_h : 0) * p.q.h, __builtin_amdgcn_readfirstlane(there ? q_limit : 0u));
+        const u32x4 Dres = head_rsrc(gdo + (size_t)b * p.dout.b + (size_t)(there ? next_h : 0) * p.dout.h, __builtin_amdgcn_readfirstlane(there ? do_limit : 0u));
+        const uint32_t at = (uint32_t)(u & 1) * Tile::PAIR;
+        w.issue(Qres, next_row, at, q_bytes);
+        w.issue(Dres, next_row, at + Tile::TILE, do_bytes);
+        if (w.wave == 0) {
+          const int row = next_row + w.l32;
+          stat = w.g == 0 ? INFINITY : 0.f;  // a row that is not there, or sees nothing: exponents of -inf
           if (there && row < seen.end) {
-            const size_t from = ((size_t)b * p.Hq + h) * p.Nq + row;
-            if (w.wave == 0) {
+            const size_t from = ((size_t)b * p.Hq + next_h) * p.Nq + row;
+            if (w.g == 0) {
               const float z = lse[from];
               if (z != -INFINITY) stat = z * 1.4426950408889634f - GradScale<T>::P_LOG2;
             } else {
@@ -330,113 +424,159 @@ __global__ __launch_bounds__(256, NB == 2 ? 1 : 2) void window_attn_dkv_kernel(
             }
           }
         }
+        next_row += ROWS;
+        if (next_row >= seen.end) {
+          next_row = seen.begin;
+          ++next_h;
+        }
       };
       auto leave_stat = [&](int u) {
-        if (w.wave < 2) stats[(u & 1) * 128 + w.wave * 64 + w.lane] = stat;
+        if (w.wave == 0) stats[(u & 1) * 64 + w.lane] = stat;
       };
+      const int first_row = next_row;
       issue(u0);
-      u32x4 k[NB][DS], v[NB][DS];
-      int from[NB], to[NB];  // queries that see the column's key
+      u32x4 k[DS], v[DS];  // (k: unused where it stays in LDS)
+      const int key = min(col, j1 - 1);
+      const size_t kv_head = (size_t)b * p.kv.b + (size_t)hk * p.kv.h;
+      uint32_t at_k = 0;
+      if constexpr (K_LDS) {  // the wave's own rows, in pieces of 1 KB
+        const uint32_t kv_bytes = (uint32_t)p.kv.n * 2, keys = 2 * Tile::PAIR + 1024 + w.wave * Tile::COLS * Tile::ROWB;
+        const u32x4 Kres = head_rsrc(gk + kv_head, __builtin_amdgcn_readfirstlane((uint32_t)(j1 - 1) * kv_bytes + Tile::ROWB));
+        constexpr int PER = 64 / Tile::CH;  // rows of an instruction
+        const uint32_t to_lds = __builtin_amdgcn_readfirstlane(w.lds_base + keys);
+        const int row0 = __builtin_amdgcn_readfirstlane(j0 + w.wave * Tile::COLS);
 #pragma unroll
-      for (int c = 0; c < NB; ++c) {
-        const int row = min(col[c], j1 - 1);
-        w.operand(gk + (size_t)b * p.kv.b + (size_t)hk * p.kv.h + (size_t)row * p.kv.n, k[c]);
-        w.operand(gv + (size_t)b * p.kv.b + (size_t)hk * p.kv.h + (size_t)row * p.kv.n, v[c]);
-        from[c] = WindowQueries::first_of(p, e, row);
-        to[c] = col[c] < j1 ? WindowQueries::end_of(p, e, row) : from[c];
+        for (int it = 0; it < Tile::COLS / PER; ++it) {
+          const int row = it * PER + w.lane / Tile::CH, c = (w.lane % Tile::CH) ^ both_swz<D>(row);
+          dma_16B_per_lane<true>(Kres, (uint32_t)(w.lane / Tile::CH) * kv_bytes + c * 16, (uint32_t)(row0 + it * PER) * kv_bytes, to_lds + it * 1024);
+        }
+        at_k = w.second_addr + w.lds_base + keys;
+      } else {
+        w.operand(gk + kv_head + (size_t)key * p.kv.n, k);
+        Tile::arrive(k);
       }
-      // every key of the wave is seen by the queries [from_max, to_min)
-      const int jw0 = j0 + __builtin_amdgcn_readfirstlane(w.wave) * Tile::COLS, jw1 = jw0 + Tile::COLS;
+      w.operand(gv + kv_head + (size_t)key * p.kv.n, v);
+      // queries that see the column's key, and those that see every key of the wave
+      const int from = WindowQueries::first_of(p, e, key), to = col < j1 ? WindowQueries::end_of(p, e, key) : from;
+      const int jw0 = __builtin_amdgcn_readfirstlane(j0 + w.wave * Tile::COLS), jw1 = jw0 + Tile::COLS;
       const int from_max = jw1 <= j1 ? WindowQueries::first_of(p, e, jw1 - 1) : INT_MAX;
       const int to_min = jw1 <= p.sinks ? e.q_len : WindowQueries::end_of(p, e, max(jw0, p.sinks));
+      Tile::arrive(v);
       leave_stat(u0);
-      const float sc = p.scale_log2e;
+      const float sc = p.scale_log2e == 0.f ? 1e-30f : p.scale_log2e, unseen = sc < 0.f ? INFINITY : -INFINITY;
+      int first = first_row;
       for (int u = u0; u < u1; ++u) {
         asm volatile("s_waitcnt vmcnt(0)" : : : "memory");
         __syncthreads();  // tile u and its rows' lse and delta are there, and every wave is done with tile u - 1
         issue(u + 1);
-        const char *const qt = lds + (u & 1) * 2 * Tile::TILE, *const dt = qt + Tile::TILE;
-        const float *const st = stats + (u & 1) * 128;
-        const int first = seen.begin + 64 * (u % n_tiles);
-        const bool whole = first >= from_max && first + 64 <= to_min;
-#pragma unroll
-        for (int half = 0; half < 2; ++half) {
-          f32x16 s[NB], dp[NB];
-          uint32_t pp[NB][8], ds[NB][8];
-          float lse2[16], dl[16];
-          w.products(qt, half, k, s);
-          w.products(dt, half, v, dp);
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const int at = 32 * half + 16 * (i >> 1) + 8 * w.g + 4 * (i & 1);
-            const f32x4 x = *reinterpret_cast<const f32x4 *>(st + at), y = *reinterpret_cast<const f32x4 *>(st + 64 + at);
-#pragma unroll
-            for (int n = 0; n < 4; ++n) lse2[4 * i + n] = x[n], dl[4 * i + n] = y[n];
+        // S, dP, dV, dK; exponentials and dS beside them from dP on
+        constexpr int PH = Tile::PH, N = 4 * DS;
+        constexpr int RING = D == 128 ? 4 : 8, STAT_AHEAD = 3;  // pairs of lse2, then of delta, on their way
+        f32x16 s, dp;
+        u32x4 pp[2], ds[2], a[3], second[3];
+        f32x2 row_stat[RING];
+        const typename Tile::Places at(w, w.lds_base + (uint32_t)(u & 1) * Tile::PAIR);
+        uint32_t at_second = at_k;
+        asm volatile("" : "+v"(at_second));
+        const float *const row_stats = stats + (u & 1) * 64 + 8 * w.g;
+        auto fetch = [&](auto q) {
+          constexpr int i = q;
+          if constexpr (i < DS) {
+            a[i % 3] = Tile::rows_of(at.rows, 0, i);
+            if constexpr (K_LDS) second[i % 3] = Tile::rows_of(at_second, 0, i);
+          } else if constexpr (i < 2 * DS) {
+            a[i % 3] = Tile::rows_of(at.rows, Tile::TILE, i - DS);
+          } else {
+            constexpr int n = (i - 2 * DS) % DS;
+            a[i % 3] = Tile::cols_of(at.cols, i < 3 * DS ? Tile::TILE : 0, n / DB, n % DB);
           }
+        };
+        fetch(std::integral_constant<int, 0>{});
+        fetch(std::integral_constant<int, 1>{});
+        static_unroll<N>([&](auto gap) {
+          constexpr int g = gap;
+          if constexpr (g + 2 < N) fetch(std::integral_constant<int, g + 2>{});
+          static_unroll<16>([&](auto r) {
+            constexpr int pair = r % 8, use = PH + (r < 8 ? Tile::exp_gap(pair) : Tile::ds_gap(pair));
+            if constexpr (use - STAT_AHEAD == g)
+              row_stat[r % RING] = *reinterpret_cast<const f32x2 *>(row_stats + (r < 8 ? 0 : 32) + 16 * (pair >> 2) + 2 * (pair & 3));
+          });
+          if constexpr (g < DS) {
+            if constexpr (K_LDS) mfma_gap<T, true, g == 0>(s, a[g % 3], second[g % 3]);
+            else mfma_gap<T, true, g == 0>(s, a[g % 3], k[g]);
+          } else if constexpr (g < 2 * DS) {
+            mfma_gap<T, true, g == DS>(dp, a[g % 3], v[g - DS]);
+          } else if constexpr (g < 3 * DS) {
+            mfma_gap<T, false, false>(dv[(g - 2 * DS) % DB], a[g % 3], pp[(g - 2 * DS) / DB]);
+          } else {
+            mfma_gap<T, false, false>(dk[(g - 3 * DS) % DB], a[g % 3], ds[(g - 3 * DS) / DB]);
+          }
+          if constexpr (g == PH) {
+            settle<true>(s);
+            if (!(first >= from_max && first + ROWS <= to_min)) {  // queries that do not see the column's key
+              const int begin = first + 8 * w.g - from;
+              const uint32_t span = (uint32_t)max(to - from, 0);
 #pragma unroll
-          for (int c = 0; c < NB; ++c) {
-            if (!whole) {
-              const int at = first + 32 * half + 8 * w.g - from[c];
-              const uint32_t span = (uint32_t)max(to[c] - from[c], 0);
-#pragma unroll
-              for (int n = 0; n < 16; ++n) s[c][n] = (uint32_t)(at + 16 * (n >> 3) + (n & 7)) < span ? s[c][n] * sc : -INFINITY;
-            } else {
-#pragma unroll
-              for (int n = 0; n < 16; ++n) s[c][n] *= sc;
-            }
-#pragma unroll
-            for (int n = 0; n < 16; n += 2) {
-              const float p0 = __builtin_amdgcn_exp2f(s[c][n] - lse2[n]), p1 = __builtin_amdgcn_exp2f(s[c][n + 1] - lse2[n + 1]);
-              pp[c][n >> 1] = T::pack(p0, p1);
-              ds[c][n >> 1] = T::pack(p0 * __builtin_fmaf(dp[c][n], Tile::DS_OF_P, -dl[n]),
-                                      p1 * __builtin_fmaf(dp[c][n + 1], Tile::DS_OF_P, -dl[n + 1]));
+              for (int n = 0; n < 16; ++n) s[n] = (uint32_t)(begin + 16 * (n >> 3) + (n & 7)) < span ? s[n] : unseen;
             }
           }
-          w.add(dt, half, pp, dv);
-          w.add(qt, half, ds, dk);
-        }
+          if constexpr (g == PH + Tile::EXP_GAPS) settle<true>(dp);
+          static_unroll<Tile::UNITS>([&](auto u_) {
+            constexpr int n = 2 * u_;
+            if constexpr (PH + Tile::exp_gap(u_) == g) {
+              const f32x2 lse2 = row_stat[u_ % RING];
+              s[n] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[n], sc, -lse2[0]));
+              s[n + 1] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[n + 1], sc, -lse2[1]));
+              pp[n >> 3][(n >> 1) & 3] = T::pack(s[n], s[n + 1]);
+            }
+            if constexpr (PH + Tile::ds_gap(u_) == g) {
+              const f32x2 dl = row_stat[(8 + u_) % RING];
+              ds[n >> 3][(n >> 1) & 3] = T::pack(s[n] * __builtin_fmaf(dp[n], Tile::DS_OF_P, -dl[0]), s[n + 1] * __builtin_fmaf(dp[n + 1], Tile::DS_OF_P, -dl[1]));
+            }
+          });
+          __builtin_amdgcn_sched_barrier(0);
+        });
         leave_stat(u + 1);
+        first += ROWS;
+        if (first >= seen.end) first = seen.begin;
       }
       asm volatile("s_waitcnt vmcnt(0)" : : : "memory");
+#pragma unroll
+      for (int db = 0; db < DB; ++db) {
+        settle<false>(dk[db]);
+        settle<false>(dv[db]);
+      }
     }
   }
-  const float fk = p.scale / GradScale<T>::DS, fv = Tile::P_UNIT;
+  if (col >= p.Nk) return;
   if (parts > 1) {
     // sums of a part: [part][dk, dv][key rows][D], the blocks with sinks behind all others
     const size_t rows = (size_t)p.B * p.Hkv * p.Nk, sink_rows = (size_t)p.B * p.Hkv * p.n_sink_blocks * BKV;
-    const size_t first = p.bwd_parts > 1 && sink_block ? (size_t)p.bwd_parts * 2 * rows : 0;
+    const size_t before = p.bwd_parts > 1 && sink_block ? (size_t)p.bwd_parts * 2 * rows : 0;
     const size_t n = sink_block ? sink_rows : rows;
+    const size_t row = sink_block ? (size_t)bh * p.n_sink_blocks * BKV + col : (size_t)bh * p.Nk + col;
+    float *const to_k = p.part_dkv + (before + (size_t)(2 * part) * n + row) * D + 4 * w.g, *const to_v = to_k + n * D;
 #pragma unroll
-    for (int c = 0; c < NB; ++c)
-      if (col[c] < p.Nk) {
-        const size_t row = sink_block ? (size_t)bh * p.n_sink_blocks * BKV + col[c] : (size_t)bh * p.Nk + col[c];
-        float *const to_k = p.part_dkv + (first + (size_t)(2 * part) * n + row) * D + 4 * w.g, *const to_v = to_k + n * D;
+    for (int db = 0; db < DB; ++db)
 #pragma unroll
-        for (int db = 0; db < DB; ++db)
-#pragma unroll
-          for (int a = 0; a < 4; ++a) {
-            *reinterpret_cast<f32x4 *>(to_k + 32 * db + 8 * a) = f32x4{dk[c][db][4 * a], dk[c][db][4 * a + 1], dk[c][db][4 * a + 2], dk[c][db][4 * a + 3]};
-            *reinterpret_cast<f32x4 *>(to_v + 32 * db + 8 * a) = f32x4{dv[c][db][4 * a], dv[c][db][4 * a + 1], dv[c][db][4 * a + 2], dv[c][db][4 * a + 3]};
-          }
+      for (int a = 0; a < 4; ++a) {
+        *reinterpret_cast<f32x4 *>(to_k + 32 * db + 8 * a) = f32x4{dk[db][4 * a], dk[db][4 * a + 1], dk[db][4 * a + 2], dk[db][4 * a + 3]};
+        *reinterpret_cast<f32x4 *>(to_v + 32 * db + 8 * a) = f32x4{dv[db][4 * a], dv[db][4 * a + 1], dv[db][4 * a + 2], dv[db][4 * a + 3]};
       }
     return;
   }
-#pragma unroll
-  for (int c = 0; c < NB; ++c)
-    if (col[c] < p.Nk) {
-      const bool there = col[c] < j1;  // rows behind the keys: zeros, their columns repeat the last key
-      const size_t at = (size_t)b * p.dkv.b + (size_t)hk * p.dkv.h + (size_t)col[c] * p.dkv.n;
-      Tile::store(dk[c], fk, there, gdk + at, w.g);
-      Tile::store(dv[c], fv, there, gdv + at, w.g);
-    }
+  const bool there = col < j1;  // rows behind the keys: zeros, their columns repeat the last key
+  const size_t at = (size_t)b * p.dkv.b + (size_t)hk * p.dkv.h + (size_t)col * p.dkv.n;
+  Tile::store(dk, p.scale / GradScale<T>::DS, there, gdk + at, w.g);
+  Tile::store(dv, Tile::P_UNIT, there, gdv + at, w.g);
 }
 
 // Sums of the parts of every key's row, in the order of the parts, rounded once.
-template <int D, int NB, typename T>
+template <int D, typename T>
 __global__ __launch_bounds__(256) void window_attn_dkv_sum_kernel(uint16_t *__restrict__ gdk, uint16_t *__restrict__ gdv,
                                                                   const WindowDims p) {
-  using Tile = GradTile<D, NB, T>;
-  constexpr int LANES = D / 8, BKV = 4 * Tile::COLS;
+  using Tile = GradTile<D, T>;
+  constexpr int LANES = D / 8, BKV = Tile::BLOCK;
   const size_t rows = (size_t)p.B * p.Hkv * p.Nk;
   // with whole blocks beside those with sinks, only the rows of the latter are left to be added up
   const int cut = p.bwd_parts > 1 ? p.Nk : min(p.Nk, p.n_sink_blocks * BKV);

@@ -114,32 +114,40 @@ int launch_forward(const uint16_t *q, const uint16_t *k, const uint16_t *v, uint
 }
 
 // ---- gradients ----------------------------------------------------------------------------------------------
-// How the gradients' kernels are cut: blocks of 32 columns per wave of either kernel, and the parts that the queries of a
-// block of keys are cut into.  A block with sinks is seen by all later queries, so it gets parts as long as the others'.
+// How the queries that see a block of 128 keys are cut into parts.  A block with sinks is seen by all later queries, so it
+// gets parts as long as the others'.
 struct GradPlan {
-  int nb_q, nb_k, parts, sink_parts, sink_blocks;
+  int parts, sink_parts, sink_blocks;
   int64_t bytes;  // of the workspace: delta, and the sums of the parts
 };
 GradPlan grad_plan(int B, int Hq, int Hkv, int Nq, int Nk, int D, const calibatt_window &w) {
   GradPlan g;
-  g.nb_q = (int64_t)B * Hq * ((Nq + 255) / 256) >= WINDOW_CUS ? 2 : 1;
-  g.nb_k = (int64_t)B * Hkv * ((Nk + 255) / 256) >= WINDOW_CUS / 2 ? 2 : 1;
-  const int block = 128 * g.nb_k, blocks = (Nk + block - 1) / block;
-  g.sink_blocks = w.left < 0 ? 0 : (std::min(w.sinks, Nk) + block - 1) / block;
-  const int64_t G = Hq / Hkv, heads = (int64_t)B * Hkv;
-  const int64_t all = G * ((Nq + 63) / 64);
+  constexpr int BLOCK = 128, ROWS = 32, SLOTS = 2 * WINDOW_CUS;
+  const int64_t blocks = (Nk + BLOCK - 1) / BLOCK, G = Hq / Hkv, heads = (int64_t)B * Hkv;
+  g.sink_blocks = w.left < 0 ? 0 : (std::min(w.sinks, Nk) + BLOCK - 1) / BLOCK;
+  const int64_t all = G * ((Nq + ROWS - 1) / ROWS);
   int64_t one = all;  // tiles of queries that see a block, without sinks
-  if (w.left >= 0 && w.right >= 0) one = std::min<int64_t>(all, G * (window_span(w, block, Nq) + 63) / 64);
-  const int64_t total = heads * (g.sink_blocks * all + (blocks - g.sink_blocks) * one);
-  const int64_t slots = WINDOW_CUS * (g.nb_k == 2 ? 1 : 2);
-  // a third of an even share, so that the last parts end close to each other, but no short ones
-  const int64_t length = std::max<int64_t>({1, std::min<int64_t>(16, one), total / (3 * slots)});
-  g.parts = (int)std::min<int64_t>(WINDOW_MAX_PARTS, std::max<int64_t>(1, one / length));
-  g.sink_parts = (int)std::min<int64_t>(WINDOW_MAX_PARTS, std::max<int64_t>(1, all / std::max<int64_t>(1, one / g.parts)));
+  if (w.left >= 0 && w.right >= 0) one = std::min<int64_t>(all, G * ((window_span(w, BLOCK, Nq) + ROWS - 1) / ROWS));
+  // Rounds of workgroups times the length of a part, which costs so many tiles beside its own (its start, its sums to
+  // memory and back).
+  constexpr int64_t PART_COST = 12, ALONE = 4;
+  double best = 0.0;
+  g.parts = 0;
+  for (int64_t parts = 1; parts <= WINDOW_MAX_PARTS && (parts == 1 || one / parts >= 8); ++parts) {
+    const int64_t length = (one + parts - 1) / parts;
+    const int64_t sink_parts = std::min<int64_t>(WINDOW_MAX_PARTS, (all + length - 1) / length);
+    const int64_t sink_length = (all + sink_parts - 1) / sink_parts, longest = g.sink_blocks ? std::max(length, sink_length) : length;
+    const int64_t units = heads * (g.sink_blocks * sink_parts + (blocks - g.sink_blocks) * parts);
+    const double cost = (double)((units + SLOTS - 1) / SLOTS) * (double)(longest + (parts > 1 ? PART_COST : ALONE));
+    if (g.parts && cost >= 0.97 * best) continue;
+    best = cost;
+    g.parts = (int)parts;
+    g.sink_parts = (int)std::max<int64_t>(1, sink_parts);
+  }
   g.bytes = ((int64_t)B * Hq * Nq + 3) / 4 * 16;
   const int64_t row = 2 * D * 4;
   if (g.parts > 1) g.bytes += g.parts * heads * Nk * row;
-  if (g.sink_blocks && g.sink_parts > 1) g.bytes += g.sink_parts * heads * g.sink_blocks * block * row;
+  if (g.sink_blocks && g.sink_parts > 1) g.bytes += g.sink_parts * heads * g.sink_blocks * BLOCK * row;
   return g;
 }
 
@@ -150,41 +158,25 @@ struct GradTensors {
   float *delta;
 };
 
-template <int D, int NB, typename T>
-int launch_dq(const GradTensors &t, const WindowDims &p, hipStream_t stream) {
-  using Tile = GradTile<D, NB, T>;
-  static DevInfo info;
+template <int D, typename T>
+int launch_backward(const GradTensors &t, const WindowDims &p, hipStream_t stream) {
+  constexpr int BLOCK = GradTile<D, T>::BLOCK, DQ_LDS = dq_lds_bytes<D, T>(), DKV_LDS = dkv_lds_bytes<D, T>();
+  static DevInfo dq_info, dkv_info;
   int unused = 0;
-  if (int st = prepare(window_attn_dq_kernel<D, NB, T>, 256, Tile::LDS_BYTES, info, unused)) return st;
-  const int64_t units = (int64_t)p.B * p.Hq * ((p.Nq + 128 * NB - 1) / (128 * NB));
-  return launch_kernel(window_attn_dq_kernel<D, NB, T>, (unsigned)(8 * ((units + 7) / 8)), 256, Tile::LDS_BYTES, stream, t.dout,
-                       t.q, t.k, t.v, t.out, t.lse, t.dq, t.delta, p);
-}
-
-template <int D, int NB, typename T>
-int launch_dkv(const GradTensors &t, const WindowDims &p, hipStream_t stream) {
-  using Tile = GradTile<D, NB, T>;
-  constexpr int SMEM = Tile::LDS_BYTES + 1024, BLOCK = 128 * NB;
-  static DevInfo info;
-  int unused = 0;
-  if (int st = prepare(window_attn_dkv_kernel<D, NB, T>, 256, SMEM, info, unused)) return st;
-  const int blocks = (p.Nk + BLOCK - 1) / BLOCK;
-  const int64_t units = (int64_t)p.B * p.Hkv * ((int64_t)p.n_sink_blocks * p.bwd_sink_parts + (int64_t)(blocks - p.n_sink_blocks) * p.bwd_parts);
-  if (units > 0x7ffffff0LL) return CALIBATT_ERR_SHAPE;
-  if (int st = launch_kernel(window_attn_dkv_kernel<D, NB, T>, (unsigned)(8 * ((units + 7) / 8)), 256, SMEM, stream, t.dout, t.q,
+  if (int st = prepare(window_attn_dq_kernel<D, T>, 256, DQ_LDS, dq_info, unused)) return st;
+  if (int st = prepare(window_attn_dkv_kernel<D, T>, 256, DKV_LDS, dkv_info, unused)) return st;
+  const int64_t q_units = (int64_t)p.B * p.Hq * ((p.Nq + BLOCK - 1) / BLOCK), blocks = (p.Nk + BLOCK - 1) / BLOCK;
+  const int64_t k_units = (int64_t)p.B * p.Hkv * (p.n_sink_blocks * p.bwd_sink_parts + (blocks - p.n_sink_blocks) * p.bwd_parts);
+  const int64_t cut = p.bwd_parts > 1 ? p.Nk : p.bwd_sink_parts > 1 ? std::min(p.Nk, p.n_sink_blocks * BLOCK) : 0;
+  const int64_t per_wg = 256 / (D / 8), sum_wgs = (2 * cut * p.B * p.Hkv + per_wg - 1) / per_wg;
+  if (q_units > 0x7ffffff0LL || k_units > 0x7ffffff0LL || sum_wgs > 0x7fffffffLL) return CALIBATT_ERR_SHAPE;
+  if (int st = launch_kernel(window_attn_dq_kernel<D, T>, (unsigned)(8 * ((q_units + 7) / 8)), 256, DQ_LDS, stream, t.dout, t.q, t.k,
+                             t.v, t.out, t.lse, t.dq, t.delta, p))
+    return st;
+  if (int st = launch_kernel(window_attn_dkv_kernel<D, T>, (unsigned)(8 * ((k_units + 7) / 8)), 256, DKV_LDS, stream, t.dout, t.q,
                              t.k, t.v, t.lse, (const float *)t.delta, t.dk, t.dv, p))
     return st;
-  const int64_t cut = p.bwd_parts > 1 ? p.Nk : p.bwd_sink_parts > 1 ? std::min(p.Nk, p.n_sink_blocks * BLOCK) : 0;
-  const int64_t rows = 2 * cut * p.B * p.Hkv, per_wg = 256 / (D / 8);
-  if (rows == 0) return CALIBATT_OK;
-  if ((rows + per_wg - 1) / per_wg > 0x7fffffff) return CALIBATT_ERR_SHAPE;
-  return launch_kernel(window_attn_dkv_sum_kernel<D, NB, T>, (unsigned)((rows + per_wg - 1) / per_wg), 256, 0, stream, t.dk, t.dv, p);
-}
-
-template <int D, typename T>
-int launch_backward(const GradTensors &t, const WindowDims &p, const GradPlan &g, hipStream_t stream) {
-  if (int st = g.nb_q == 2 ? launch_dq<D, 2, T>(t, p, stream) : launch_dq<D, 1, T>(t, p, stream)) return st;
-  return g.nb_k == 2 ? launch_dkv<D, 2, T>(t, p, stream) : launch_dkv<D, 1, T>(t, p, stream);
+  return sum_wgs ? launch_kernel(window_attn_dkv_sum_kernel<D, T>, (unsigned)sum_wgs, 256, 0, stream, t.dk, t.dv, p) : CALIBATT_OK;
 }
 
 }  // namespace
@@ -264,6 +256,6 @@ extern "C" int calibatt_window_attn_bwd(const void *dout, const void *q, const v
   const GradTensors t = {(const uint16_t *)dout, (const uint16_t *)q, (const uint16_t *)k, (const uint16_t *)v,
                          (const uint16_t *)out, lse, (uint16_t *)dq, (uint16_t *)dk, (uint16_t *)dv, (float *)workspace};
   hipStream_t s = (hipStream_t)stream;
-  if (D == 128) return dtype == CALIBATT_BF16 ? launch_backward<128, Bf16>(t, p, g, s) : launch_backward<128, F16>(t, p, g, s);
-  return dtype == CALIBATT_BF16 ? launch_backward<64, Bf16>(t, p, g, s) : launch_backward<64, F16>(t, p, g, s);
+  if (D == 128) return dtype == CALIBATT_BF16 ? launch_backward<128, Bf16>(t, p, s) : launch_backward<128, F16>(t, p, s);
+  return dtype == CALIBATT_BF16 ? launch_backward<64, Bf16>(t, p, s) : launch_backward<64, F16>(t, p, s);
 }
