@@ -101,6 +101,17 @@ __device__ __forceinline__ void dma_16B_per_lane(const u32x4 rsrc, uint32_t voff
   }
 }
 
+// The same with 4 bytes per lane: lane i's land at LDS byte address lds_off + 4 * i.
+__device__ __forceinline__ void dma_4B_per_lane(const u32x4 rsrc, uint32_t voff, uint32_t lds_off) {
+  asm volatile(
+      "s_mov_b32 m0, %0\n\t"
+      "s_nop 0\n\t"
+      "buffer_load_dword %1, %2, 0 offen lds"
+      :
+      : "s"(lds_off), "v"(voff), "s"(rsrc)
+      : "m0");
+}
+
 // Stream one ROWS x D bf16 tile global -> LDS.  Each instruction fills 1 KB of
 // LDS; LDS chunk (row, c') receives global chunk (row, c' ^ swz(row)).
 template <int D, int ROWS, int NT, bool FOR_V>

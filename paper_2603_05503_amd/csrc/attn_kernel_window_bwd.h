@@ -8,12 +8,11 @@
 //
 // Both are the same shape.  A wave owns 32 columns (its queries, or its keys) as second operands; tiles of 32 rows of two
 // matrices (K and V, or Q and dO) pass through LDS, read row-wise for S^T and dP^T (first operand: rows of the tile) and
-// transposed for the products that add up, whose second operands are P and dS as they lie in registers.  128 columns to a
-// workgroup, two workgroups per CU.
+// transposed for the products that add up, whose second operands are P and dS as they lie in registers.  Two waves per SIMD.
 //
 // A wave issues in order, an instruction every four cycles at best, and an MFMA that finds the matrix pipe busy holds up
 // what stands behind it.  So the work on 32 rows is written as a stream of GAPS: an MFMA, the read of the first operand of
-// two gaps later, a share of the vector work (exponentials beside dP and what follows it, dS behind them), a scheduling
+// three gaps later, a share of the vector work (exponentials beside dP and what follows it, dS behind them), a scheduling
 // barrier; the second wave of the SIMD fills what one leaves.  Us of dQ, and of dK and dV, for 16 380 tokens, 8 query heads
 // on 4 key heads, D = 128, nine frames of 780 and the first: scheduled by the compiler, 64 columns to a wave, one wave per
 // SIMD 930 and 2660 (it gathers reads and vector work and spills), the same in gaps 787 and 1253 (half its cycles waits),
@@ -65,13 +64,15 @@ __device__ __forceinline__ void settle(f32x16 &x) {
   else asm volatile("s_nop 15" : "+a"(x));
 }
 
-template <int D, typename T>
+template <int D, typename T, int NT_>
 struct GradTile {
-  static constexpr int NT = 256, COLS = 32, BLOCK = 4 * COLS;    // columns of a wave, of the workgroup
+  static constexpr int NT = NT_, COLS = 32, BLOCK = NT / 64 * COLS;  // columns of a wave, of the workgroup
   static constexpr int ROWS = 32, ROWB = D * 2, CH = D / 8, DS = D / 16, DB = D / 32;
   static constexpr int TILE = ROWS * ROWB, PAIR = 2 * TILE;      // bytes of one matrix's tile, of both
-  static constexpr int RPI = NT / CH, ITERS = ROWS / RPI, LOADS = 2 * ITERS;  // load instructions of a wave for a pair
-  static_assert(RPI % 16 == 0, "the swizzle of an instruction's rows is the same for every one");
+  // Load instructions of a wave for a pair of tiles: ITERS for each matrix, or, where one instruction of half the waves
+  // fills a tile, one for the matrix of its half.
+  static constexpr int ITERS = ROWS * CH / NT, LOADS = ITERS ? 2 * ITERS : 1, RPI = NT / CH;
+  static_assert((ITERS && RPI % 16 == 0) || 2 * ROWS * CH == NT, "the swizzle of an instruction's rows is the same for every one");
   static constexpr float P_UNIT = GradScale<T>::P_LOG2 == 0.f ? 1.f : 1.f / 32768.f;  // what P_LOG2 stands for
   static constexpr float DS_OF_P = GradScale<T>::DS * P_UNIT;                         // factor of dP - delta beside P as kept
 
@@ -79,6 +80,7 @@ struct GradTile {
   // values, by their gap behind the start of dP: exponentials over 22/16 of a phase, then each pair's dS, in dK and dV's
   // kernel over 18/16, in dQ's over the 10/16 that are left before S of the next rows.  In the former the first halves are
   // needed half a phase before the second ones: probabilities from gap PH on (dV), dS from gap 2 PH on (dK).
+  static constexpr int AHEAD = 3, RA = AHEAD + 1;  // gaps between the read of a first operand and its use
   static constexpr int PH = DS, UNITS = 8, EXP_GAPS = 22 * PH / 16;
   static_assert(DS == 2 * DB, "phases of the same length");
   static constexpr int exp_gap(int u) { return u * EXP_GAPS / UNITS; }
@@ -93,15 +95,18 @@ struct GradTile {
   uint32_t col_addr[2];  // transposed reads: d block db at col_addr[t] ^ (db << 6), slab j at + 16 j * ROWB
   uint32_t second_addr;  // operands of columns that stay in LDS: chunk column s at second_addr ^ (s << 5)
   uint32_t lds_base, lds_wave;
+  int load_row, load_chunk;  // what this lane loads of a tile
 
   __device__ __forceinline__ explicit GradTile(char *lds) {
     tid = threadIdx.x;
     lane = tid & 63;
-    wave = tid >> 6;
+    wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     l32 = lane & 31;
     g = lane >> 5;
     lds_base = (uint32_t)(uintptr_t)(LDS_PTR(char))lds;  // a multiple of 1024
-    lds_wave = __builtin_amdgcn_readfirstlane(lds_base + wave * 1024);
+    lds_wave = __builtin_amdgcn_readfirstlane(lds_base + wave * 1024);  // (of a pair, where a load is half a pair)
+    load_row = tid / CH % ROWS;
+    load_chunk = (tid % CH) ^ both_swz<D>(load_row);
     const int row = (l32 & 0x13) | ((l32 & 4) << 1) | ((l32 & 8) >> 1);  // so that a lane's eight values are of consecutive rows
     row_addr = row * ROWB + ((g ^ both_swz<D>(row)) << 4);
     second_addr = l32 * ROWB + ((g ^ both_swz<D>(l32)) << 4);
@@ -112,13 +117,20 @@ struct GradTile {
       col_addr[t] = r * ROWB + (((2 * (blk & 1) + ((L16 & 3) >> 1)) ^ both_swz<D>(r)) << 4) + (L16 & 1) * 8;
     }
   }
-  // rows [row0, row0 + 32) of a matrix into the tile at LDS byte `at`
-  __device__ __forceinline__ void issue(const u32x4 rsrc, int row0, uint32_t at, uint32_t row_bytes) const {
-    const int row = tid / CH, c = (tid % CH) ^ both_swz<D>(row);
-    const uint32_t voff = row * row_bytes + c * 16;
+  // rows [row0, row0 + 32) of two matrices into the pair of tiles at LDS byte `at`
+  __device__ __forceinline__ void issue(const u32x4 first, const u32x4 second, int row0, uint32_t at, uint32_t first_bytes, uint32_t second_bytes) const {
+    if constexpr (ITERS > 0) {
 #pragma unroll
-    for (int it = 0; it < ITERS; ++it)
-      dma_16B_per_lane<true>(rsrc, voff, (uint32_t)(row0 + it * RPI) * row_bytes, lds_wave + at + it * NT * 16);
+      for (int it = 0; it < ITERS; ++it)
+        dma_16B_per_lane<true>(first, load_row * first_bytes + load_chunk * 16, (uint32_t)(row0 + it * RPI) * first_bytes, lds_wave + at + it * NT * 16);
+#pragma unroll
+      for (int it = 0; it < ITERS; ++it)
+        dma_16B_per_lane<true>(second, load_row * second_bytes + load_chunk * 16, (uint32_t)(row0 + it * RPI) * second_bytes, lds_wave + at + TILE + it * NT * 16);
+    } else if (wave < NT / 128) {
+      dma_16B_per_lane<true>(first, load_row * first_bytes + load_chunk * 16, (uint32_t)row0 * first_bytes, lds_wave + at);
+    } else {
+      dma_16B_per_lane<true>(second, load_row * second_bytes + load_chunk * 16, (uint32_t)row0 * second_bytes, lds_wave + at);
+    }
   }
   // a column's D elements as second operand
   __device__ __forceinline__ void operand(const uint16_t *row, u32x4 (&x)[DS]) const {
@@ -166,18 +178,22 @@ struct GradTile {
 };
 
 // ---- dQ -----------------------------------------------------------------------------------------------------
-// The tiles lie in four buffers: in its turn tile t is read for dP, t - 1 for dQ and t + 1 for S, while t + 2 is on its way.
+// 128 queries to a workgroup, two workgroups per CU: eight waves of one workgroup on the same tiles read them half as often,
+// but wait for each other (655 us two, 700 one, also with a barrier for every second tile and three tiles on their way).
+// The tiles lie in a ring of four: in its turn tile t is read for dP, t - 1 for dQ and t + 1 for S, while t + 2 is on its way.
 template <int D, typename T>
-constexpr int dq_lds_bytes() { return 4 * GradTile<D, T>::PAIR; }
+using DqTile = GradTile<D, T, 256>;
+template <int D, typename T>
+constexpr int dq_lds_bytes() { return 4 * DqTile<D, T>::PAIR; }
 
 template <int D, typename T>
 __global__ __launch_bounds__(256, 2) void window_attn_dq_kernel(
     const uint16_t *__restrict__ gdo, const uint16_t *__restrict__ gq, const uint16_t *__restrict__ gk,
     const uint16_t *__restrict__ gv, const uint16_t *__restrict__ gout, const float *__restrict__ lse,
-    uint16_t *__restrict__ gdq, float *__restrict__ delta, const WindowDims p) {
-  using Tile = GradTile<D, T>;
+    uint16_t *__restrict__ gdq, float *__restrict__ stats, const WindowDims p) {
+  using Tile = DqTile<D, T>;
   using Tiles = WindowTiles<Tile::ROWS>;
-  constexpr int BQ = Tile::BLOCK, DS = Tile::DS, DB = Tile::DB;
+  constexpr int BQ = Tile::BLOCK, DS = Tile::DS, DB = Tile::DB, AHEAD = Tile::AHEAD, RA = Tile::RA;
   extern __shared__ __attribute__((aligned(1024))) char lds[];
   const int nbq = (p.Nq + BQ - 1) / BQ;
   const int unit = window_unit(p.B * p.Hq * nbq);
@@ -201,9 +217,7 @@ __global__ __launch_bounds__(256, 2) void window_attn_dq_kernel(
       const int end = t < tiles.n ? tiles.end(t) : 0;
       Kres[2] = Vres[2] = __builtin_amdgcn_readfirstlane(end > 0 ? (uint32_t)(end - 1) * row_bytes + Tile::ROWB : 0u);
       const int first = __builtin_amdgcn_readfirstlane(t < tiles.n ? tiles.row(t) : 0);
-      const uint32_t at = (uint32_t)(t & 3) * Tile::PAIR;
-      w.issue(Kres, first, at, row_bytes);
-      w.issue(Vres, first, at + Tile::TILE, row_bytes);
+      w.issue(Kres, Vres, first, (uint32_t)(t & 3) * Tile::PAIR, row_bytes, row_bytes);
     };
     issue(0);
     u32x4 q[DS], dout[DS];
@@ -231,8 +245,11 @@ __global__ __launch_bounds__(256, 2) void window_attn_dq_kernel(
           dl = __builtin_fmaf(x2[1], y2[1], dl);
         }
       dl = sum_with_other_half(dl);
-      if (w.g == 0 && col < i1) delta[row0 + col] = dl;
       dl *= Tile::DS_OF_P;
+      if (w.g == 0 && col < i1) {  // for dK and dV: [head][lse2, delta][query]
+        stats[2 * row0 + col] = lse2;
+        stats[2 * row0 + p.Nq + col] = dl;
+      }
     }
     // dO in AGPRs, beside dQ: the compiler halves the registers, and the VGPRs are for the rest
     Tile::arrive(q);
@@ -240,7 +257,7 @@ __global__ __launch_bounds__(256, 2) void window_attn_dq_kernel(
     // the logit of an unseen key: -inf behind its product with the scale, which is not zero
     const float sc = p.scale_log2e == 0.f ? 1e-30f : p.scale_log2e, unseen = sc < 0.f ? INFINITY : -INFINITY;
     f32x16 s, dp;
-    u32x4 ds[2], ds_before[2], a[3];
+    u32x4 ds[2], ds_before[2], a[RA];
     ds_before[0] = ds_before[1] = u32x4{0, 0, 0, 0};
     issue(1);
     asm volatile("s_waitcnt vmcnt(%0)" : : "n"(Tile::LOADS) : "memory");
@@ -251,31 +268,30 @@ __global__ __launch_bounds__(256, 2) void window_attn_dq_kernel(
       a[0] = Tile::rows_of(before.rows, 0, k);
       mfma_gap<T, true, k == 0>(s, a[0], q[k]);
     });
-    a[0] = Tile::rows_of(before.rows, Tile::TILE, 0);
-    a[1] = Tile::rows_of(before.rows, Tile::TILE, 1);
+    static_unroll<AHEAD>([&](auto i) { a[i] = Tile::rows_of(before.rows, Tile::TILE, i); });
     for (int t = 0; t < tiles.n; ++t) {
       // dP, dQ of tile t - 1, S of tile t + 1; exponentials and dS beside the first two
       const typename Tile::Places at = place_of(t), next = place_of(t + 1);
       constexpr int N = 3 * DS;
-      static_assert(N % 3 == 0, "the operands' places go on with the next tile");
+      static_assert(N % RA == 0, "the operands' places go on with the next tile");
       auto fetch = [&](auto q) {  // the operand of gap q (behind the last one: of tile t + 1)
         constexpr int i = q;
-        if constexpr (i < DS) a[i % 3] = Tile::rows_of(at.rows, Tile::TILE, i);
-        else if constexpr (i < 2 * DS) a[i % 3] = Tile::cols_of(before.cols, 0, (i - DS) / DB, (i - DS) % DB);
-        else if constexpr (i < N) a[i % 3] = Tile::rows_of(next.rows, 0, i - 2 * DS);
-        else a[i % 3] = Tile::rows_of(next.rows, Tile::TILE, i - N);
+        if constexpr (i < DS) a[i % RA] = Tile::rows_of(at.rows, Tile::TILE, i);
+        else if constexpr (i < 2 * DS) a[i % RA] = Tile::cols_of(before.cols, 0, (i - DS) / DB, (i - DS) % DB);
+        else if constexpr (i < N) a[i % RA] = Tile::rows_of(next.rows, 0, i - 2 * DS);
+        else a[i % RA] = Tile::rows_of(next.rows, Tile::TILE, i - N);
       };
       static_unroll<N>([&](auto gap) {
         constexpr int g = gap;
-        if constexpr (g == 2 * DS - 2) {
+        if constexpr (g == 2 * DS - AHEAD) {
           asm volatile("s_waitcnt vmcnt(0)" : : : "memory");
           __syncthreads();  // tile t + 1 is there, and every wave is done with tile t - 2, whose place t + 2 takes
           issue(t + 2);
         }
-        fetch(std::integral_constant<int, g + 2>{});
-        if constexpr (g < DS) mfma_gap<T, true, g == 0, true>(dp, a[g % 3], dout[g]);
-        else if constexpr (g < 2 * DS) mfma_gap<T, false, false>(dq[(g - DS) % DB], a[g % 3], ds_before[(g - DS) / DB]);
-        else mfma_gap<T, true, g == 2 * DS>(s, a[g % 3], q[g - 2 * DS]);
+        fetch(std::integral_constant<int, g + AHEAD>{});
+        if constexpr (g < DS) mfma_gap<T, true, g == 0, true>(dp, a[g % RA], dout[g]);
+        else if constexpr (g < 2 * DS) mfma_gap<T, false, false>(dq[(g - DS) % DB], a[g % RA], ds_before[(g - DS) / DB]);
+        else mfma_gap<T, true, g == 2 * DS>(s, a[g % RA], q[g - 2 * DS]);
         if constexpr (g == 0) {
           settle<true>(s);
           if (!tiles.whole(t)) {  // the keys that a query does not see: a probability of 2^-inf
@@ -352,23 +368,26 @@ __device__ __forceinline__ int grad_units(const WindowDims &p, int n_blocks) {
 // K stay in LDS there, where reading them takes the reads of 32 rows from 32 to 40 KB a wave.
 template <int D>
 constexpr bool DKV_K_IN_LDS = D == 128;
+constexpr int DKV_RING = 4;  // two tiles that are read, two on their way
+template <int D, typename T>
+using DkvTile = GradTile<D, T, 512>;
 template <int D, typename T>
 constexpr int dkv_lds_bytes() {
-  using Tile = GradTile<D, T>;
-  return 2 * Tile::PAIR + 1024 + (DKV_K_IN_LDS<D> ? Tile::BLOCK * Tile::ROWB : 0);
+  using Tile = DkvTile<D, T>;
+  return DKV_RING * Tile::PAIR + DKV_RING * 256 + (DKV_K_IN_LDS<D> ? Tile::BLOCK * Tile::ROWB : 0);
 }
 
 template <int D, typename T>
-__global__ __launch_bounds__(256, 2) void window_attn_dkv_kernel(
+__global__ __launch_bounds__(512, 2) void window_attn_dkv_kernel(
     const uint16_t *__restrict__ gdo, const uint16_t *__restrict__ gq, const uint16_t *__restrict__ gk,
-    const uint16_t *__restrict__ gv, const float *__restrict__ lse, const float *__restrict__ delta,
+    const uint16_t *__restrict__ gv, const float *__restrict__ stats,
     uint16_t *__restrict__ gdk, uint16_t *__restrict__ gdv, const WindowDims p) {
-  using Tile = GradTile<D, T>;
-  constexpr int BKV = Tile::BLOCK, DS = Tile::DS, DB = Tile::DB, ROWS = Tile::ROWS;
+  using Tile = DkvTile<D, T>;
+  constexpr int BKV = Tile::BLOCK, DS = Tile::DS, DB = Tile::DB, ROWS = Tile::ROWS, AHEAD = Tile::AHEAD, RA = Tile::RA;
   constexpr bool K_LDS = DKV_K_IN_LDS<D>;
   extern __shared__ __attribute__((aligned(1024))) char lds[];
-  // [2 buffers][Q, dO tiles], [2 buffers][lse2 of 32 rows, delta of 32 rows], K of the block
-  float *const stats = reinterpret_cast<float *>(lds + 2 * Tile::PAIR);
+  // [ring][Q, dO tiles], [ring][lse2 of 32 rows, delta of 32 rows], K of the block
+  constexpr int STATS = DKV_RING * Tile::PAIR, KEYS = STATS + DKV_RING * 256;
   const int nkb = (p.Nk + BKV - 1) / BKV, per_head = grad_units(p, nkb);
   const int unit = window_unit(p.B * p.Hkv * per_head);
   if (unit < 0) return;
@@ -401,46 +420,40 @@ __global__ __launch_bounds__(256, 2) void window_attn_dkv_kernel(
     if (u0 < u1) {
       const uint32_t q_bytes = (uint32_t)p.q.n * 2, do_bytes = (uint32_t)p.dout.n * 2;
       const uint32_t q_limit = (uint32_t)(seen.end - 1) * q_bytes + Tile::ROWB, do_limit = (uint32_t)(seen.end - 1) * do_bytes + Tile::ROWB;
-      // the tile that is asked for next: its head and first row; and of wave 0's lanes the lse or delta of a row of it
-      int next_h = __builtin_amdgcn_readfirstlane(hk * G + u0 / n_tiles), next_row = __builtin_amdgcn_readfirstlane(seen.begin + ROWS * (u0 % n_tiles));
-      float stat = 0.f;
-      auto issue = [&](int u) {
+      // the tile that is asked for next: its head's rows, and the first of them
+      int next_row = __builtin_amdgcn_readfirstlane(seen.begin + ROWS * (u0 % n_tiles));
+      const int h0 = __builtin_amdgcn_readfirstlane(hk * G + u0 / n_tiles);
+      const uint16_t *next_q = gq + (size_t)b * p.q.b + (size_t)h0 * p.q.h, *next_do = gdo + (size_t)b * p.dout.b + (size_t)h0 * p.dout.h;
+      const float *next_stats = stats + 2 * ((size_t)b * p.Hq + h0) * p.Nq;
+      const uint32_t stats_limit = (uint32_t)p.Nq * 8;  // bytes of a head's, 2^28 at most as its rows are within 2^32
+      auto issue = [&](int u) {  // a tile behind the last one reads nothing
         const bool there = u < u1;
-        const u32x4 Qres = head_rsrc(gq + (size_t)b * p.q.b + (size_t)(there ? next_h : 0) * p.q.h, __builtin_amdgcn_readfirstlane(there ? q_limit : 0u));
-        const u32x4 Dres = head_rsrc(gdo + (size_t)b * p.dout.b + (size_t)(there ? next_h : 0) * p.dout.h, __builtin_amdgcn_readfirstlane(there ? do_limit : 0u));
-        const uint32_t at = (uint32_t)(u & 1) * Tile::PAIR;
-        w.issue(Qres, next_row, at, q_bytes);
-        w.issue(Dres, next_row, at + Tile::TILE, do_bytes);
-        if (w.wave == 0) {
+        const u32x4 Qres = head_rsrc(next_q, __builtin_amdgcn_readfirstlane(there ? q_limit : 0u));
+        const u32x4 Dres = head_rsrc(next_do, __builtin_amdgcn_readfirstlane(there ? do_limit : 0u));
+        w.issue(Qres, Dres, next_row, (uint32_t)(u % DKV_RING) * Tile::PAIR, q_bytes, do_bytes);
+        if (w.wave == 0) {  // lanes 0..31 lse2 of the rows, lanes 32..63 delta; zeros behind the last query
+          const u32x4 Sres = head_rsrc(reinterpret_cast<const uint16_t *>(next_stats), __builtin_amdgcn_readfirstlane(there ? stats_limit : 0u));
           const int row = next_row + w.l32;
-          stat = w.g == 0 ? INFINITY : 0.f;  // a row that is not there, or sees nothing: exponents of -inf
-          if (there && row < seen.end) {
-            const size_t from = ((size_t)b * p.Hq + next_h) * p.Nq + row;
-            if (w.g == 0) {
-              const float z = lse[from];
-              if (z != -INFINITY) stat = z * 1.4426950408889634f - GradScale<T>::P_LOG2;
-            } else {
-              stat = delta[from] * Tile::DS_OF_P;
-            }
-          }
+          dma_4B_per_lane(Sres, row < seen.end ? (uint32_t)(row + (w.g ? p.Nq : 0)) * 4 : 0xfffffff0u,  // (behind every limit)
+                          __builtin_amdgcn_readfirstlane(w.lds_base + STATS + (uint32_t)(u % DKV_RING) * 256));
         }
         next_row += ROWS;
         if (next_row >= seen.end) {
           next_row = seen.begin;
-          ++next_h;
+          next_q += p.q.h;
+          next_do += p.dout.h;
+          next_stats += 2 * (size_t)p.Nq;
         }
       };
-      auto leave_stat = [&](int u) {
-        if (w.wave == 0) stats[(u & 1) * 64 + w.lane] = stat;
-      };
-      const int first_row = next_row;
+      int first = next_row;
       issue(u0);
+      issue(u0 + 1);
       u32x4 k[DS], v[DS];  // (k: unused where it stays in LDS)
       const int key = min(col, j1 - 1);
       const size_t kv_head = (size_t)b * p.kv.b + (size_t)hk * p.kv.h;
       uint32_t at_k = 0;
       if constexpr (K_LDS) {  // the wave's own rows, in pieces of 1 KB
-        const uint32_t kv_bytes = (uint32_t)p.kv.n * 2, keys = 2 * Tile::PAIR + 1024 + w.wave * Tile::COLS * Tile::ROWB;
+        const uint32_t kv_bytes = (uint32_t)p.kv.n * 2, keys = KEYS + w.wave * Tile::COLS * Tile::ROWB;
         const u32x4 Kres = head_rsrc(gk + kv_head, __builtin_amdgcn_readfirstlane((uint32_t)(j1 - 1) * kv_bytes + Tile::ROWB));
         constexpr int PER = 64 / Tile::CH;  // rows of an instruction
         const uint32_t to_lds = __builtin_amdgcn_readfirstlane(w.lds_base + keys);
@@ -462,54 +475,56 @@ __global__ __launch_bounds__(256, 2) void window_attn_dkv_kernel(
       const int from_max = jw1 <= j1 ? WindowQueries::first_of(p, e, jw1 - 1) : INT_MAX;
       const int to_min = jw1 <= p.sinks ? e.q_len : WindowQueries::end_of(p, e, max(jw0, p.sinks));
       Tile::arrive(v);
-      leave_stat(u0);
       const float sc = p.scale_log2e == 0.f ? 1e-30f : p.scale_log2e, unseen = sc < 0.f ? INFINITY : -INFINITY;
-      int first = first_row;
       for (int u = u0; u < u1; ++u) {
-        asm volatile("s_waitcnt vmcnt(0)" : : : "memory");
-        __syncthreads();  // tile u and its rows' lse and delta are there, and every wave is done with tile u - 1
-        issue(u + 1);
+        if (((u - u0) & 1) == 0) {
+          asm volatile("s_waitcnt vmcnt(0)" : : : "memory");
+          __syncthreads();  // tiles u and u + 1 (and K) are there, and every wave is done with the two before, whose places
+          issue(u + 2);     // the next two take
+          issue(u + 3);
+        }
         // S, dP, dV, dK; exponentials and dS beside them from dP on
         constexpr int PH = Tile::PH, N = 4 * DS;
         constexpr int RING = D == 128 ? 4 : 8, STAT_AHEAD = 3;  // pairs of lse2, then of delta, on their way
         f32x16 s, dp;
-        u32x4 pp[2], ds[2], a[3], second[3];
+        u32x4 pp[2], ds[2], a[RA], second[RA];
         f32x2 row_stat[RING];
-        const typename Tile::Places at(w, w.lds_base + (uint32_t)(u & 1) * Tile::PAIR);
+        const typename Tile::Places at(w, w.lds_base + (uint32_t)(u % DKV_RING) * Tile::PAIR);
         uint32_t at_second = at_k;
         asm volatile("" : "+v"(at_second));
-        const float *const row_stats = stats + (u & 1) * 64 + 8 * w.g;
+        const float *const row_stats = reinterpret_cast<const float *>(lds + STATS + (u % DKV_RING) * 256) + 8 * w.g;
         auto fetch = [&](auto q) {
           constexpr int i = q;
           if constexpr (i < DS) {
-            a[i % 3] = Tile::rows_of(at.rows, 0, i);
-            if constexpr (K_LDS) second[i % 3] = Tile::rows_of(at_second, 0, i);
+            a[i % RA] = Tile::rows_of(at.rows, 0, i);
+            if constexpr (K_LDS) second[i % RA] = Tile::rows_of(at_second, 0, i);
           } else if constexpr (i < 2 * DS) {
-            a[i % 3] = Tile::rows_of(at.rows, Tile::TILE, i - DS);
+            a[i % RA] = Tile::rows_of(at.rows, Tile::TILE, i - DS);
           } else {
             constexpr int n = (i - 2 * DS) % DS;
-            a[i % 3] = Tile::cols_of(at.cols, i < 3 * DS ? Tile::TILE : 0, n / DB, n % DB);
+            a[i % RA] = Tile::cols_of(at.cols, i < 3 * DS ? Tile::TILE : 0, n / DB, n % DB);
           }
         };
-        fetch(std::integral_constant<int, 0>{});
-        fetch(std::integral_constant<int, 1>{});
+        static_unroll<AHEAD>(fetch);
         static_unroll<N>([&](auto gap) {
           constexpr int g = gap;
-          if constexpr (g + 2 < N) fetch(std::integral_constant<int, g + 2>{});
+          if constexpr (g + AHEAD < N) fetch(std::integral_constant<int, g + AHEAD>{});
           static_unroll<16>([&](auto r) {
-            constexpr int pair = r % 8, use = PH + (r < 8 ? Tile::exp_gap(pair) : Tile::ds_gap(pair));
+            constexpr auto use_of = [](int x) { return PH + (x < 8 ? Tile::exp_gap(x) : Tile::ds_gap(x % 8)); };
+            constexpr int pair = r % 8, use = use_of(r);
+            static_assert(r < RING || use_of(r - RING) < use - STAT_AHEAD, "the place of a pair of rows is free again");
             if constexpr (use - STAT_AHEAD == g)
               row_stat[r % RING] = *reinterpret_cast<const f32x2 *>(row_stats + (r < 8 ? 0 : 32) + 16 * (pair >> 2) + 2 * (pair & 3));
           });
           if constexpr (g < DS) {
-            if constexpr (K_LDS) mfma_gap<T, true, g == 0>(s, a[g % 3], second[g % 3]);
-            else mfma_gap<T, true, g == 0>(s, a[g % 3], k[g]);
+            if constexpr (K_LDS) mfma_gap<T, true, g == 0>(s, a[g % RA], second[g % RA]);
+            else mfma_gap<T, true, g == 0>(s, a[g % RA], k[g]);
           } else if constexpr (g < 2 * DS) {
-            mfma_gap<T, true, g == DS>(dp, a[g % 3], v[g - DS]);
+            mfma_gap<T, true, g == DS>(dp, a[g % RA], v[g - DS]);
           } else if constexpr (g < 3 * DS) {
-            mfma_gap<T, false, false>(dv[(g - 2 * DS) % DB], a[g % 3], pp[(g - 2 * DS) / DB]);
+            mfma_gap<T, false, false>(dv[(g - 2 * DS) % DB], a[g % RA], pp[(g - 2 * DS) / DB]);
           } else {
-            mfma_gap<T, false, false>(dk[(g - 3 * DS) % DB], a[g % 3], ds[(g - 3 * DS) / DB]);
+            mfma_gap<T, false, false>(dk[(g - 3 * DS) % DB], a[g % RA], ds[(g - 3 * DS) / DB]);
           }
           if constexpr (g == PH) {
             settle<true>(s);
@@ -536,7 +551,6 @@ __global__ __launch_bounds__(256, 2) void window_attn_dkv_kernel(
           });
           __builtin_amdgcn_sched_barrier(0);
         });
-        leave_stat(u + 1);
         first += ROWS;
         if (first >= seen.end) first = seen.begin;
       }
@@ -575,7 +589,7 @@ __global__ __launch_bounds__(256, 2) void window_attn_dkv_kernel(
 template <int D, typename T>
 __global__ __launch_bounds__(256) void window_attn_dkv_sum_kernel(uint16_t *__restrict__ gdk, uint16_t *__restrict__ gdv,
                                                                   const WindowDims p) {
-  using Tile = GradTile<D, T>;
+  using Tile = DkvTile<D, T>;
   constexpr int LANES = D / 8, BKV = Tile::BLOCK;
   const size_t rows = (size_t)p.B * p.Hkv * p.Nk;
   // with whole blocks beside those with sinks, only the rows of the latter are left to be added up

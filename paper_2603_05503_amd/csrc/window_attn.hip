@@ -114,15 +114,15 @@ int launch_forward(const uint16_t *q, const uint16_t *k, const uint16_t *v, uint
 }
 
 // ---- gradients ----------------------------------------------------------------------------------------------
-// How the queries that see a block of 128 keys are cut into parts.  A block with sinks is seen by all later queries, so it
+// How the queries that see a block of 256 keys are cut into parts.  A block with sinks is seen by all later queries, so it
 // gets parts as long as the others'.
 struct GradPlan {
   int parts, sink_parts, sink_blocks;
-  int64_t bytes;  // of the workspace: delta, and the sums of the parts
+  int64_t bytes;  // of the workspace: lse and delta of every query, and the sums of the parts
 };
 GradPlan grad_plan(int B, int Hq, int Hkv, int Nq, int Nk, int D, const calibatt_window &w) {
   GradPlan g;
-  constexpr int BLOCK = 128, ROWS = 32, SLOTS = 2 * WINDOW_CUS;
+  constexpr int BLOCK = 256, ROWS = 32, SLOTS = WINDOW_CUS;
   const int64_t blocks = (Nk + BLOCK - 1) / BLOCK, G = Hq / Hkv, heads = (int64_t)B * Hkv;
   g.sink_blocks = w.left < 0 ? 0 : (std::min(w.sinks, Nk) + BLOCK - 1) / BLOCK;
   const int64_t all = G * ((Nq + ROWS - 1) / ROWS);
@@ -144,7 +144,7 @@ GradPlan grad_plan(int B, int Hq, int Hkv, int Nq, int Nk, int D, const calibatt
     g.parts = (int)parts;
     g.sink_parts = (int)std::max<int64_t>(1, sink_parts);
   }
-  g.bytes = ((int64_t)B * Hq * Nq + 3) / 4 * 16;
+  g.bytes = ((int64_t)B * Hq * Nq + 1) / 2 * 16;
   const int64_t row = 2 * D * 4;
   if (g.parts > 1) g.bytes += g.parts * heads * Nk * row;
   if (g.sink_blocks && g.sink_parts > 1) g.bytes += g.sink_parts * heads * g.sink_blocks * BLOCK * row;
@@ -155,26 +155,26 @@ struct GradTensors {
   const uint16_t *dout, *q, *k, *v, *out;
   const float *lse;
   uint16_t *dq, *dk, *dv;
-  float *delta;
+  float *stats;  // lse and delta as the second kernel wants them, [head][2][query]
 };
 
 template <int D, typename T>
 int launch_backward(const GradTensors &t, const WindowDims &p, hipStream_t stream) {
-  constexpr int BLOCK = GradTile<D, T>::BLOCK, DQ_LDS = dq_lds_bytes<D, T>(), DKV_LDS = dkv_lds_bytes<D, T>();
+  constexpr int BLOCK_Q = DqTile<D, T>::BLOCK, BLOCK = DkvTile<D, T>::BLOCK, DQ_LDS = dq_lds_bytes<D, T>(), DKV_LDS = dkv_lds_bytes<D, T>();
   static DevInfo dq_info, dkv_info;
   int unused = 0;
   if (int st = prepare(window_attn_dq_kernel<D, T>, 256, DQ_LDS, dq_info, unused)) return st;
-  if (int st = prepare(window_attn_dkv_kernel<D, T>, 256, DKV_LDS, dkv_info, unused)) return st;
-  const int64_t q_units = (int64_t)p.B * p.Hq * ((p.Nq + BLOCK - 1) / BLOCK), blocks = (p.Nk + BLOCK - 1) / BLOCK;
+  if (int st = prepare(window_attn_dkv_kernel<D, T>, 512, DKV_LDS, dkv_info, unused)) return st;
+  const int64_t q_units = (int64_t)p.B * p.Hq * ((p.Nq + BLOCK_Q - 1) / BLOCK_Q), blocks = (p.Nk + BLOCK - 1) / BLOCK;
   const int64_t k_units = (int64_t)p.B * p.Hkv * (p.n_sink_blocks * p.bwd_sink_parts + (blocks - p.n_sink_blocks) * p.bwd_parts);
   const int64_t cut = p.bwd_parts > 1 ? p.Nk : p.bwd_sink_parts > 1 ? std::min(p.Nk, p.n_sink_blocks * BLOCK) : 0;
   const int64_t per_wg = 256 / (D / 8), sum_wgs = (2 * cut * p.B * p.Hkv + per_wg - 1) / per_wg;
   if (q_units > 0x7ffffff0LL || k_units > 0x7ffffff0LL || sum_wgs > 0x7fffffffLL) return CALIBATT_ERR_SHAPE;
   if (int st = launch_kernel(window_attn_dq_kernel<D, T>, (unsigned)(8 * ((q_units + 7) / 8)), 256, DQ_LDS, stream, t.dout, t.q, t.k,
-                             t.v, t.out, t.lse, t.dq, t.delta, p))
+                             t.v, t.out, t.lse, t.dq, t.stats, p))
     return st;
-  if (int st = launch_kernel(window_attn_dkv_kernel<D, T>, (unsigned)(8 * ((k_units + 7) / 8)), 256, DKV_LDS, stream, t.dout, t.q,
-                             t.k, t.v, t.lse, (const float *)t.delta, t.dk, t.dv, p))
+  if (int st = launch_kernel(window_attn_dkv_kernel<D, T>, (unsigned)(8 * ((k_units + 7) / 8)), 512, DKV_LDS, stream, t.dout, t.q,
+                             t.k, t.v, (const float *)t.stats, t.dk, t.dv, p))
     return st;
   return sum_wgs ? launch_kernel(window_attn_dkv_sum_kernel<D, T>, (unsigned)sum_wgs, 256, 0, stream, t.dk, t.dv, p) : CALIBATT_OK;
 }
@@ -252,7 +252,7 @@ extern "C" int calibatt_window_attn_bwd(const void *dout, const void *q, const v
   p.bwd_parts = g.parts;
   p.bwd_sink_parts = g.sink_parts;
   p.n_sink_blocks = g.sink_blocks;
-  p.part_dkv = (float *)workspace + ((int64_t)B * Hq * Nq + 3) / 4 * 4;
+  p.part_dkv = (float *)workspace + ((int64_t)B * Hq * Nq + 1) / 2 * 4;
   const GradTensors t = {(const uint16_t *)dout, (const uint16_t *)q, (const uint16_t *)k, (const uint16_t *)v,
                          (const uint16_t *)out, lse, (uint16_t *)dq, (uint16_t *)dk, (uint16_t *)dv, (float *)workspace};
   hipStream_t s = (hipStream_t)stream;
