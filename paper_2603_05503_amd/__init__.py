@@ -47,4 +47,4 @@ from .binding import (  # noqa: F401
     vote_masks,
 )
 from .layer_ops import RotaryAxes, Window, layer_norm_bwd, layer_norm_fwd, rope_axes, window_attn_bwd, window_attn_fwd  # noqa: F401,E402
-from .pipeline import CalibAttention, CalibrationResult, Calibrator, load_calibration, save_calibration  # noqa: F401,E402
+from .pipeline import CalibAttention, CalibrationResult, Calibrator, QKPreparation, load_calibration, save_calibration  # noqa: F401,E402

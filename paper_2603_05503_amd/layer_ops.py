@@ -60,6 +60,19 @@ def _dtype_of(t):
     return _dtypes.get(t.dtype)
 
 
+# What the checks of a call found, and the arguments that follow from shapes, strides and element types alone, by exactly
+# these: a small call's time is the host's, and checking and laying them out again takes a third of it (q and k of two
+# heads of 1024 tokens 11.3 us, with this 9.0; nothing of a tensor's memory or identity is kept).
+_plans = {}
+
+
+def _remember(key, plan):
+    if len(_plans) >= 1024:
+        _plans.clear()
+    _plans[key] = plan
+    return plan
+
+
 def _on(device):
     """Context in which ``device`` is the current one: kernels are launched on the current device."""
     import torch
@@ -123,22 +136,6 @@ class RotaryAxes:
         self._c = _CRope(n, 1 if interleaved else 0, (C.c_int32 * 4)(*self.dims), (C.c_int32 * 4)(*self.lengths),
                          self.table.data_ptr())
         self._c_at = C.addressof(self._c)
-        self._grids = {}  # (grid, start) -> struct
-
-    def _place(self, grid, start, positions):
-        if positions is not None:
-            return _CRopePlace((C.c_int32 * 4)(), (C.c_int32 * 4)(), positions.data_ptr(),
-                               positions.stride(0) if positions.dim() == 3 else 0)
-        key = (tuple(grid), tuple(start))
-        place = self._grids.get(key)
-        if place is None:
-            n = len(self.dims)
-            if len(key[0]) != n or len(key[1]) != n:
-                raise ValueError(f"grid and start have one entry per axis ({n})")
-            if len(self._grids) >= 64:  # a stream's start moves on: old places are of no use
-                self._grids.clear()
-            place = self._grids[key] = _CRopePlace((C.c_int32 * 4)(*key[0]), (C.c_int32 * 4)(*key[1]), None, 0)
-        return place
 
 
 def rope_axes(q, k, rope: RotaryAxes, grid=None, start=None, positions=None, q_out=None, k_out=None, inverse: bool = False,
@@ -151,51 +148,70 @@ def rope_axes(q, k, rope: RotaryAxes, grid=None, start=None, positions=None, q_o
     leaves the axis's channels as they are, one behind the table's length gives NaN.  ``inverse`` turns back: with it the
     call takes a gradient of its outputs to that of its inputs.  ``q_out=q, k_out=k`` turns in place."""
     lib = _b.load_library()
-    shape, dtype = q.shape, _dtype_of(q)
-    if not (q.is_cuda and dtype is not None and len(shape) == 4 and q.stride(3) == 1):
-        raise ValueError("q must be a bf16, fp16 or fp32 CUDA tensor [B, H, N, D] with contiguous D")
-    if k is not None and not (k.dtype == q.dtype and k.device == q.device and k.dim() == 4 and k.stride(3) == 1
-                              and k.shape[0] == shape[0] and k.shape[2:] == shape[2:]):
-        raise ValueError("k must have q's element type, device and shape but for the heads, with contiguous D")
-    if (grid is None) == (positions is None):
-        raise ValueError("either a grid or positions")
-    if positions is None:
-        start = (0,) * len(rope.dims) if start is None else start
-    else:
-        import torch
-
-        n = len(rope.dims)
-        if start is not None:
-            raise ValueError("start belongs to a grid")
-        if not (positions.device == q.device and positions.dtype == torch.int32
-                and tuple(positions.shape) in ((shape[2], n), (shape[0], shape[2], n))
-                and positions.stride(-1) == 1 and positions.stride(-2) == n):
-            raise ValueError(f"positions must be an int32 CUDA tensor [N, {n}] or [B, N, {n}] with contiguous rows")
-    if rope.table.device != q.device:
-        raise ValueError("the tables of the axes are on another device")
-    stream, other = _b._stream_of(stream, q.device)
-    for x, x_out in ((q, q_out), (k, k_out)):
-        if x_out is not None and (x is None or not (x_out.shape == x.shape and x_out.dtype == x.dtype and x_out.device == x.device
-                                                    and x_out.stride(3) == 1)):
-            raise ValueError("an output must have its input's shape, element type and device, with contiguous D")
-    with _on(q.device):
+    device = q.device
+    key = ("rope", rope.dims, rope.lengths, q.shape, q.stride(), q.dtype, k is not None and (k.shape, k.stride(), k.dtype), q.is_cuda,
+           q_out is not None and (q_out.shape, q_out.stride(), q_out.dtype),
+           k_out is not None and (k_out.shape, k_out.stride(), k_out.dtype),
+           positions is not None and (positions.shape, positions.stride(), positions.dtype),
+           None if grid is None else tuple(grid), None if start is None else tuple(start))
+    plan = _plans.get(key)
+    if plan is None:
+        plan = _rope_plan(key, q, k, rope, grid, start, positions, q_out, k_out)
+    for t in (rope.table, k, q_out, k_out, positions):
+        if t is not None and t.device != device:
+            raise ValueError("all tensors, and the tables of the axes, must be on one device")
+    place, dims, dtype, keep, at = plan
+    stream, other = _b._stream_of(stream, device)
+    with _on(device):
         if q_out is None:
             q_out = _empty_like(q, other)
         if k is not None and k_out is None:
             k_out = _empty_like(k, other)
-        place = rope._place(grid, start, positions)
-        if k is None:
-            keep, at = _strides(q, q_out)
-            at += [None, None]
-            hk, kp, kop = 0, None, None
-        else:
-            keep, at = _strides(q, q_out, k, k_out)
-            hk, kp, kop = k.shape[1], k.data_ptr(), k_out.data_ptr()
-        st = lib.calibatt_rope_axes(q.data_ptr(), q_out.data_ptr(), kp, kop, shape[0], shape[1], hk, shape[2], shape[3],
-                                    rope._c_at, C.addressof(place), *at, dtype, 1 if inverse else 0, stream)
+        if place is None:
+            place = _CRopePlace((C.c_int32 * 4)(), (C.c_int32 * 4)(), positions.data_ptr(),
+                                positions.stride(0) if positions.dim() == 3 else 0)
+        st = lib.calibatt_rope_axes(q.data_ptr(), q_out.data_ptr(), None if k is None else k.data_ptr(),
+                                    None if k is None else k_out.data_ptr(), *dims, rope._c_at, C.addressof(place), *at, dtype,
+                                    1 if inverse else 0, stream)
     if st != 0:
         raise _b.CalibattError(st, "calibatt_rope_axes")
     return q_out, k_out
+
+
+def _rope_plan(key, q, k, rope, grid, start, positions, q_out, k_out):
+    """Checks of a ``rope_axes`` call; (place or None, sizes, element type, array of strides, their addresses)."""
+    import torch
+
+    shape, dtype, n = q.shape, _dtype_of(q), len(rope.dims)
+    if not (q.is_cuda and dtype is not None and len(shape) == 4 and q.stride(3) == 1):
+        raise ValueError("q must be a bf16, fp16 or fp32 CUDA tensor [B, H, N, D] with contiguous D")
+    if k is not None and not (k.dtype == q.dtype and k.dim() == 4 and k.stride(3) == 1 and k.shape[0] == shape[0]
+                              and k.shape[2:] == shape[2:]):
+        raise ValueError("k must have q's element type and shape but for the heads, with contiguous D")
+    if (grid is None) == (positions is None):
+        raise ValueError("either a grid or positions")
+    place = None
+    if positions is None:
+        grid, start = tuple(grid), (0,) * n if start is None else tuple(start)
+        if len(grid) != n or len(start) != n:
+            raise ValueError(f"grid and start have one entry per axis ({n})")
+        place = _CRopePlace((C.c_int32 * 4)(*grid), (C.c_int32 * 4)(*start), None, 0)
+    elif start is not None:
+        raise ValueError("start belongs to a grid")
+    elif not (positions.is_cuda and positions.dtype == torch.int32
+              and tuple(positions.shape) in ((shape[2], n), (shape[0], shape[2], n))
+              and positions.stride(-1) == 1 and positions.stride(-2) == n):
+        raise ValueError(f"positions must be an int32 CUDA tensor [N, {n}] or [B, N, {n}] with contiguous rows")
+    for x, x_out in ((q, q_out), (k, k_out)):
+        if x_out is not None and (x is None or not (x_out.shape == x.shape and x_out.dtype == x.dtype and x_out.stride(3) == 1)):
+            raise ValueError("an output must have its input's shape and element type, with contiguous D")
+    # a new output is dense, with its input's order of axes
+    tensors = [q, q_out if q_out is not None else torch.empty_like(q, device="meta")]
+    if k is not None:
+        tensors += [k, k_out if k_out is not None else torch.empty_like(k, device="meta")]
+    keep, at = _strides(*tensors)
+    return _remember(key, (place, (shape[0], shape[1], 0 if k is None else k.shape[1], shape[2], shape[3]), dtype, keep,
+                           at + [None] * (4 - len(at))))
 
 
 def _rows(t, what):
@@ -206,22 +222,40 @@ def _rows(t, what):
     return (1,) * pad + tuple(t.shape[:-1]), (0,) * pad + t.stride()[:-1]
 
 
-def _norm_arguments(x, weight, bias, others):
-    """Checks, and (n0, n1, n2, C, strides of x and of every tensor of ``others``, their array)."""
+def _norm_plan(key, x, weight, bias, others):
+    """Checks of a layer norm's call; (n0, n1, n2, C), array of the strides of x and of every tensor of ``others`` (None: new,
+    dense, with x's order of axes), its address, element types of x and of the weight."""
+    import torch
+
     rows, s = _rows(x, "x")
     flat = list(s)
     for name, t in others:
-        if not (t.shape == x.shape and t.dtype == x.dtype and t.device == x.device):
-            raise ValueError(f"{name} must have the shape, element type and device of x")
-        flat += _rows(t, name)[1]
+        if t is None:
+            t = torch.empty_like(x, device="meta")
+        elif not (t.shape == x.shape and t.dtype == x.dtype):
+            raise ValueError(f"{name} must have the shape and element type of x")
+        else:
+            _rows(t, name)
+        flat += (0,) * (4 - t.dim()) + t.stride()[:-1]
     if bias is not None and weight is None:
         raise ValueError("a bias needs a weight")
+    dtype = _dtype_of(x)
     for t in (weight, bias):
-        if t is not None and not (t.device == x.device and tuple(t.shape) == tuple(x.shape[-1:]) and t.is_contiguous()
-                                  and _dtype_of(t) in (_dtype_of(x), 2) and t.dtype == weight.dtype):
-            raise ValueError("weight and bias must be contiguous [C] on x's device, both of x's element type or both fp32")
+        if t is not None and not (t.is_cuda and tuple(t.shape) == tuple(x.shape[-1:]) and t.is_contiguous()
+                                  and _dtype_of(t) in (dtype, 2) and t.dtype == weight.dtype):
+            raise ValueError("weight and bias must be contiguous CUDA tensors [C], both of x's element type or both fp32")
     array = (C.c_int64 * len(flat))(*flat)
-    return rows, array, C.addressof(array)
+    return _remember(key, ((*rows, x.shape[-1]), array, C.addressof(array), dtype, dtype if weight is None else _dtype_of(weight)))
+
+
+def _like(t):
+    return t is not None and (t.shape, t.stride(), t.dtype, t.is_cuda)
+
+
+def _on_one_device(device, *tensors):
+    for t in tensors:
+        if t is not None and t.device != device:
+            raise ValueError("all tensors must be on one device")
 
 
 def layer_norm_fwd(x, weight=None, bias=None, eps: float = 1e-6, center: bool = True, out=None, stream=None):
@@ -229,17 +263,17 @@ def layer_norm_fwd(x, weight=None, bias=None, eps: float = 1e-6, center: bool = 
     with a contiguous last axis).  ``weight``, ``bias``: [C] of x's element type or fp32, or None.  ``center=False``: root
     mean square, no mean is taken off.  Returns a new tensor, or ``out`` (which may be x)."""
     lib = _b.load_library()
-    if not x.is_cuda:
-        raise ValueError("x must be a CUDA tensor")
-    stream, other = _b._stream_of(stream, x.device)
-    with _on(x.device):
+    key = ("norm", _like(x), _like(weight), _like(bias), _like(out))
+    plan = _plans.get(key) or _norm_plan(key, x, weight, bias, (("out", out),))
+    sizes, keep, at, dtype, wtype = plan
+    device = x.device
+    _on_one_device(device, weight, bias, out)
+    stream, other = _b._stream_of(stream, device)
+    with _on(device):
         y = _empty_like(x, other) if out is None else out
-        rows, keep, at = _norm_arguments(x, weight, bias, (("out", y),))
-        dtype = _dtype_of(x)
         st = lib.calibatt_layer_norm_fwd(x.data_ptr(), None if weight is None else weight.data_ptr(),
-                                         None if bias is None else bias.data_ptr(), y.data_ptr(), *rows, x.shape[-1], at,
-                                         at + 24, float(eps), 1 if center else 0, dtype,
-                                         dtype if weight is None else _dtype_of(weight), stream)
+                                         None if bias is None else bias.data_ptr(), y.data_ptr(), *sizes, at, at + 24, float(eps),
+                                         1 if center else 0, dtype, wtype, stream)
     if st != 0:
         raise _b.CalibattError(st, "calibatt_layer_norm_fwd")
     return y
@@ -255,32 +289,32 @@ def layer_norm_bwd(dy, x, weight=None, bias=None, eps: float = 1e-6, center: boo
     import torch
 
     lib = _b.load_library()
-    if not x.is_cuda:
-        raise ValueError("x must be a CUDA tensor")
-    stream, other = _b._stream_of(stream, x.device)
-    with _on(x.device):
+    key = ("norm grads", _like(x), _like(dy), _like(weight), _like(bias), _like(dx))
+    plan = _plans.get(key) or _norm_plan(key, x, weight, bias, (("dy", dy), ("dx", dx)))
+    sizes, keep, at, dtype, wtype = plan
+    device = x.device
+    _on_one_device(device, dy, weight, bias, dx)
+    stream, other = _b._stream_of(stream, device)
+    with _on(device):
         to = _empty_like(x, other) if dx is None else dx
-        rows, keep, at = _norm_arguments(x, weight, bias, (("dy", dy), ("dx", to)))
-        width, dtype = x.shape[-1], _dtype_of(x)
         dweight = dbias = workspace = None
         nbytes = 0
         if weight is not None:
-            per_column = _norm_workspace_rows.get(x.device.index)
+            per_column = _norm_workspace_rows.get(device.index)
             if per_column is None:
                 n = C.c_int64(0)
                 st = lib.calibatt_layer_norm_bwd_workspace_bytes(1, C.byref(n))
                 if st != 0:
                     raise _b.CalibattError(st, "calibatt_layer_norm_bwd_workspace_bytes")
-                per_column = _norm_workspace_rows[x.device.index] = n.value
-            nbytes = per_column * width
-            workspace = _b._empty(nbytes // 4, torch.float32, x.device, other)
+                per_column = _norm_workspace_rows[device.index] = n.value
+            nbytes = per_column * sizes[3]
+            workspace = _b._empty(nbytes // 4, torch.float32, device, other)
             dweight = _empty_like(weight, other)
             dbias = None if bias is None else _empty_like(bias, other)
         st = lib.calibatt_layer_norm_bwd(dy.data_ptr(), x.data_ptr(), None if weight is None else weight.data_ptr(),
                                          to.data_ptr(), None if dweight is None else dweight.data_ptr(),
-                                         None if dbias is None else dbias.data_ptr(), *rows, width, at + 24, at, at + 48,
-                                         float(eps), 1 if center else 0, dtype,
-                                         dtype if weight is None else _dtype_of(weight),
+                                         None if dbias is None else dbias.data_ptr(), *sizes, at + 24, at, at + 48, float(eps),
+                                         1 if center else 0, dtype, wtype,
                                          None if workspace is None else workspace.data_ptr(), nbytes, stream)
     if st != 0:
         raise _b.CalibattError(st, "calibatt_layer_norm_bwd")
@@ -303,7 +337,7 @@ class Window:
         for name, v in values.items():
             if not -(2 ** 31) <= int(v) < 2 ** 31:
                 raise ValueError(f"{name} does not fit 32 bits")
-        self.left, self.right, self.sinks, self.frame, self.offset = (int(v) for v in values.values())
+        self.left, self.right, self.sinks, self.frame, self.offset = self._values = tuple(int(v) for v in values.values())
         self._bytes = {}  # sizes of a call -> workspace bytes of its forward and of its gradients
 
     def _c(self, q_start, q_len, k_len, B, device):
@@ -333,24 +367,34 @@ class Window:
         return n
 
 
-def _window_tensors(q, k, v, like_q):
-    """Checks the tensors of a call; (B, Hq, Nq, D, Hkv, Nk, dtype)."""
+def _window_plan(key, window, q, k, v, others, kv_like=()):
+    """Checks of a call; (sizes, element type, workspace bytes, array of strides, their addresses): of q, k and every tensor
+    of ``others`` (like q; None: new and dense) and ``kv_like`` (like k; None: new and dense)."""
+    import torch
+
     dtype = _dtype_of(q)
     if not (q.is_cuda and dtype in (0, 1) and q.dim() == 4 and q.stride(3) == 1):
         raise ValueError("q must be a bf16 or fp16 CUDA tensor [B, H, N, D] with contiguous D")
     B, Hq, Nq, D = q.shape
-    for name, t in like_q:
-        if not (t.shape == q.shape and t.dtype == q.dtype and t.device == q.device and t.stride(3) == 1):
-            raise ValueError(f"{name} must have the shape, element type and device of q, with contiguous D")
     for t in (k, v):
-        if not (t.dim() == 4 and t.dtype == q.dtype and t.device == q.device and t.stride(3) == 1
-                and t.shape[0] == B and t.shape[3] == D):
-            raise ValueError("k and v must be [B, Hkv, Nk, D] of q's element type and device, with contiguous D")
+        if not (t.dim() == 4 and t.dtype == q.dtype and t.stride(3) == 1 and t.shape[0] == B and t.shape[3] == D):
+            raise ValueError("k and v must be [B, Hkv, Nk, D] of q's element type, with contiguous D")
     if k.shape != v.shape or k.stride() != v.stride():
         raise ValueError("k and v must share their shape and strides")
     if k.shape[1] == 0 or Hq % k.shape[1]:
         raise ValueError("the query heads must be a multiple of the key heads")
-    return B, Hq, Nq, D, k.shape[1], k.shape[2], dtype
+    tensors = [q, k]
+    for like, names in ((q, others), (k, kv_like)):
+        for name, t in names:
+            if t is None:
+                t = torch.empty_like(like, device="meta")
+            elif not (t.shape == like.shape and t.dtype == q.dtype and t.stride(3) == 1):
+                raise ValueError(f"{name} must have the shape and element type of {'q' if like is q else 'k'}, with contiguous D")
+            tensors.append(t)
+    sizes = (B, Hq, k.shape[1], Nq, k.shape[2], D)
+    nbytes = window.workspace_bytes(*sizes)
+    keep, at = _strides(*tensors)
+    return _remember(key, (sizes, dtype, nbytes, keep, at))
 
 
 def _check_lse(lse, q):
@@ -369,23 +413,25 @@ def window_attn_fwd(q, k, v, out, window: Window, scale: float, lse=None, q_star
     import torch
 
     lib = _b.load_library()
-    B, Hq, Nq, D, Hkv, Nk, dtype = _window_tensors(q, k, v, (("out", out),))
+    device = q.device
+    key = ("window", window._values, _like(q), _like(k), _like(v), _like(out))
+    sizes, dtype, nbytes, keep, at = _plans.get(key) or _window_plan(key, window, q, k, v, (("out", out),))
+    nbytes = nbytes[0]
+    _on_one_device(device, k, v, out)
     if lse is not None:
         _check_lse(lse, q)
-    stream, other = _b._stream_of(stream, q.device)
-    c = window._c(q_start, q_len, k_len, B, q.device)
-    with _on(q.device):
-        nbytes, workspace = window.workspace_bytes(B, Hq, Hkv, Nq, Nk, D)[0], None
+    stream, other = _b._stream_of(stream, device)
+    c = window._c(q_start, q_len, k_len, sizes[0], device)
+    with _on(device):
+        workspace = None
         if nbytes:
             try:
-                workspace = _b._empty(nbytes // 4, torch.float32, q.device, other)
+                workspace = _b._empty(nbytes // 4, torch.float32, device, other)
             except torch.OutOfMemoryError:
                 pass  # whole rows, which take none
-        keep, at = _strides(q, k, out)
         st = lib.calibatt_window_attn_fwd(q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(),
-                                          None if lse is None else lse.data_ptr(), B, Hq, Hkv, Nq, Nk, D, C.addressof(c),
-                                          float(scale), *at, dtype, None if workspace is None else workspace.data_ptr(),
-                                          nbytes, stream)
+                                          None if lse is None else lse.data_ptr(), *sizes, C.addressof(c), float(scale), *at, dtype,
+                                          None if workspace is None else workspace.data_ptr(), nbytes, stream)
     if st != 0:
         raise _b.CalibattError(st, "calibatt_window_attn_fwd")
     return out
@@ -398,26 +444,27 @@ def window_attn_bwd(dout, q, k, v, out, lse, window: Window, scale: float, dq=No
     import torch
 
     lib = _b.load_library()
-    given = (("dout", dout), ("out", out)) if dq is None else (("dout", dout), ("out", out), ("dq", dq))
-    B, Hq, Nq, D, Hkv, Nk, dtype = _window_tensors(q, k, v, given)
-    _check_lse(lse, q)
     if (dk is None) != (dv is None):
         raise ValueError("dk and dv are given together")
-    stream, other = _b._stream_of(stream, q.device)
-    c = window._c(q_start, q_len, k_len, B, q.device)
-    with _on(q.device):
+    device = q.device
+    key = ("window grads", window._values, _like(q), _like(k), _like(v), _like(dout), _like(out), _like(dq), _like(dk))
+    sizes, dtype, nbytes, keep, at = _plans.get(key) or _window_plan(
+        key, window, q, k, v, (("dout", dout), ("out", out), ("dq", dq)), (("dk", dk),))
+    if dk is not None and not (dv.shape == dk.shape and dv.stride() == dk.stride() and dv.dtype == dk.dtype):
+        raise ValueError("dk and dv must share their shape, strides and element type")
+    _on_one_device(device, k, v, dout, out, dq, dk, dv)
+    _check_lse(lse, q)
+    stream, other = _b._stream_of(stream, device)
+    c = window._c(q_start, q_len, k_len, sizes[0], device)
+    at_q, at_k, at_dout, at_out, at_dq, at_dk = at
+    with _on(device):
         dq = _empty_like(q, other) if dq is None else dq
         if dk is None:
             dk, dv = _empty_like(k, other), _empty_like(k, other)
-        for t in (dk, dv):
-            if not (t.shape == k.shape and t.dtype == k.dtype and t.device == k.device and t.stride(3) == 1 and t.stride() == dk.stride()):
-                raise ValueError("dk and dv must have the shape, element type and device of k and share their strides")
-        nbytes = window.workspace_bytes(B, Hq, Hkv, Nq, Nk, D)[1]
-        workspace = _b._empty(nbytes // 4, torch.float32, q.device, other)
-        keep, at = _strides(dout, q, k, out, dq, dk)
+        workspace = _b._empty(nbytes[1] // 4, torch.float32, device, other)
         st = lib.calibatt_window_attn_bwd(dout.data_ptr(), q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), lse.data_ptr(),
-                                          dq.data_ptr(), dk.data_ptr(), dv.data_ptr(), B, Hq, Hkv, Nq, Nk, D, C.addressof(c),
-                                          float(scale), *at, dtype, workspace.data_ptr(), nbytes, stream)
+                                          dq.data_ptr(), dk.data_ptr(), dv.data_ptr(), *sizes, C.addressof(c), float(scale), at_dout, at_q,
+                                          at_k, at_out, at_dq, at_dk, dtype, workspace.data_ptr(), nbytes[1], stream)
     if st != 0:
         raise _b.CalibattError(st, "calibatt_window_attn_bwd")
     return dq, dk, dv

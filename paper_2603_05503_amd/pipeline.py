@@ -19,6 +19,7 @@ from typing import Dict, Hashable, List, Optional, Sequence, Tuple
 import numpy as np
 
 from . import binding as _b
+from . import layer_ops as _l
 
 
 @dataclass
@@ -29,13 +30,44 @@ class CalibrationResult:
     n_prompts: int
 
 
+@dataclass
+class QKPreparation:
+    """What a model does to q and k between their projection and the attention: layer norm (or root mean square) of every
+    head, then the rotation by the tokens' positions.  Each is left out where it is None."""
+    rope: Optional[_l.RotaryAxes] = None
+    grid: Optional[Tuple[int, ...]] = None      # of the rotation; None: the geometry of whoever calls
+    start: Optional[Tuple[int, ...]] = None     # position of the grid's first token
+    q_norm: Optional[Tuple] = None              # (weight, bias) of the norm, either may be None
+    k_norm: Optional[Tuple] = None
+    eps: float = 1e-6
+    center: bool = False                        # False: root mean square
+    in_place: bool = False                      # q and k are overwritten (slices of a fused projection keep their strides)
+
+    def __call__(self, q, k, geometry=None, stream=None):
+        """(q, k) prepared, on the call's stream: new tensors, or with ``in_place`` the given ones."""
+        fresh = not self.in_place
+        if self.q_norm is not None:
+            q = _l.layer_norm_fwd(q, *self.q_norm, eps=self.eps, center=self.center, out=None if fresh else q, stream=stream)
+        if self.k_norm is not None:
+            k = _l.layer_norm_fwd(k, *self.k_norm, eps=self.eps, center=self.center, out=None if fresh else k, stream=stream)
+        if self.rope is not None:
+            grid = geometry if self.grid is None else self.grid
+            if grid is None:
+                raise ValueError("a rotation needs a grid, or a caller with a geometry")
+            # what the norm made is turned where it is
+            q, k = _l.rope_axes(q, k, self.rope, grid=grid, start=self.start, stream=stream,
+                                q_out=None if fresh and self.q_norm is None else q,
+                                k_out=None if fresh and self.k_norm is None else k)
+        return q, k
+
+
 class Calibrator:
     def __init__(self, H: int, N: int, D: int, block_q: int = 128, block_k: int = 128,
                  geometry: Optional[Tuple[int, int, int]] = None, anchors: int = 5,
-                 rho: float = 0.5, gamma: float = 0.87):
+                 rho: float = 0.5, gamma: float = 0.87, prepare: Optional[QKPreparation] = None):
         self.H, self.N, self.D = H, N, D
         self.block_q, self.block_k = block_q, block_k
-        self.geometry, self.anchors, self.rho, self.gamma = geometry, anchors, rho, gamma
+        self.geometry, self.anchors, self.rho, self.gamma, self.prepare = geometry, anchors, rho, gamma, prepare
         self._counts: Dict[Hashable, object] = {}       # CUDA tensor, uint16 per block: prompts that kept it
         self._n: Dict[Hashable, int] = {}
         self._scores: Dict[Hashable, List[np.ndarray]] = {}
@@ -44,9 +76,12 @@ class Calibrator:
 
     def observe(self, key: Hashable, q, k, eps: float, scale: float) -> None:
         """One dense forward's q, k ([B, H, N, D] bf16 CUDA tensors; every batch element counts as a
-        prompt) at the step/layer ``key``, with the energy threshold ``eps`` of that step."""
+        prompt) at the step/layer ``key``, with the energy threshold ``eps`` of that step.  With ``prepare`` they come as the
+        projections leave them, and are normalised and turned first."""
         import torch
 
+        if self.prepare is not None:
+            q, k = self.prepare(q, k, self.geometry)
         # energy -> Eq. 6 -> one more vote per block, all on the device; the counters come back in finalize
         if self._energy_workspace is None or self._energy_workspace.device != q.device:
             nbytes = _b.block_energy_workspace_bytes(self.N, self.block_q, self.block_k)
@@ -123,10 +158,11 @@ class _Entry:
 class CalibAttention:
     def __init__(self, H: int, N: int, D: int, block_q: int = 128, block_k: int = 128,
                  geometry: Optional[Tuple[int, int, int]] = None, anchors: int = 5,
-                 intervals: bool = True, order: int = 4, device: str = "cuda"):
+                 intervals: bool = True, order: int = 4, device: str = "cuda", prepare: Optional[QKPreparation] = None):
         self.H, self.N, self.D = H, N, D
         self.block_q, self.block_k = block_q, block_k
         self.intervals, self.order, self.device = intervals, order, device
+        self.geometry, self.prepare = geometry, prepare
         self.entries: Dict[Hashable, _Entry] = {}
         self.amap = None
         self._anchor_workspace: Dict[Tuple[int, int, int], object] = {}
@@ -184,8 +220,12 @@ class CalibAttention:
 
     def __call__(self, q, k, v, out, key: Hashable, scale: float, stream=None):
         """One attention call of step/layer ``key``: the sparse forward on the heads of the pattern,
-        the anchor-row forward on the flagged heads; together they write every head of ``out``."""
+        the anchor-row forward on the flagged heads; together they write every head of ``out``.  With ``prepare``, q and k
+        are normalised and turned by their positions first; the prepared ones have to share v's strides (``in_place`` for
+        slices of a fused projection)."""
         e = self.entries[key]
+        if self.prepare is not None:
+            q, k = self.prepare(q, k, self.geometry, stream)
         if e.pattern is not None:
             _b.sparse_attn_fwd(q, k, v, out, e.pattern, scale, stream=stream)
         if e.head_ids is not None:
