@@ -23,8 +23,8 @@ struct WindowDims {
   Strides q, kv, out;
   int parts;                               // pieces that a block's tiles are cut into
   float *part_rows, *part_ml;              // [parts][B Hq Nq][D] sums and [parts][B Hq Nq][2] references and row sums
-  int bwd_parts, bwd_sink_parts, n_sink_blocks;  // of the gradients of k and v, see attn_kernel_window_bwd.h
-  float *part_dkv;
+  int dq_parts, bwd_parts, bwd_sink_parts, n_sink_blocks;  // of the gradients, see attn_kernel_window_bwd.h
+  float *part_dq, *part_dkv;
   Strides dout, dq, dkv;
 };
 
@@ -447,36 +447,55 @@ __global__ __launch_bounds__(STEP_WAVES * 64) void window_attn_step_kernel(
 // ---- rows that were cut -------------------------------------------------------------------------------------
 // Relative to the largest reference M of a row's parts: O = sum_s 2^(m_s - M) O_s, and likewise the row sums.  A part
 // without a visible key has a row sum of zero, and its O is not read.
-template <int D, typename T>
+// A workgroup takes ROWS rows, of each row 256 / (ROWS LANES) lanes every so many parts: one row where there are few, so that
+// its parts are read at once and not one after the other (112 rows of 31 parts, D = 128: @MERGE@).
+template <int D, int ROWS, typename T>
 __global__ __launch_bounds__(256) void window_attn_merge_kernel(uint16_t *__restrict__ gout, float *__restrict__ lse, const WindowDims p) {
-  constexpr int LANES = D / 8;
+  constexpr int LANES = D / 8, GROUPS = 256 / (ROWS * LANES);
+  __shared__ float sums[GROUPS > 1 ? GROUPS : 1][GROUPS > 1 ? ROWS * D : 1], shares[GROUPS > 1 ? GROUPS : 1][ROWS];
   const long long total = (long long)p.B * p.Hq * p.Nq;
-  const long long row = (long long)blockIdx.x * (256 / LANES) + threadIdx.x / LANES;
-  if (row >= total) return;
-  const int c = 8 * (threadIdx.x % LANES);
+  const int place = threadIdx.x / LANES, group = place / ROWS, in_wg = place % ROWS, c = 8 * (threadIdx.x % LANES);
+  const long long row = (long long)blockIdx.x * ROWS + in_wg;
+  const bool there = row < total;
   float m = -FLT_MAX, l = 0.f, x[8];
 #pragma unroll
   for (int j = 0; j < 8; ++j) x[j] = 0.f;
+  if (there) {
+#pragma unroll 8
+    for (int s = 0; s < p.parts; ++s) {
+      const f32x2 ml = *reinterpret_cast<const f32x2 *>(p.part_ml + 2 * (s * total + row));
+      if (ml[1] != 0.f) m = fmaxf(m, ml[0]);
+    }
 #pragma unroll 4
-  for (int s = 0; s < p.parts; ++s) {
-    const f32x2 ml = *reinterpret_cast<const f32x2 *>(p.part_ml + 2 * (s * total + row));
-    if (ml[1] != 0.f) m = fmaxf(m, ml[0]);
-  }
-#pragma unroll 4
-  for (int s = 0; s < p.parts; ++s) {
-    const size_t at = (size_t)(s * total + row);
-    const f32x2 ml = *reinterpret_cast<const f32x2 *>(p.part_ml + 2 * at);
-    if (ml[1] == 0.f) continue;
-    const float f = __builtin_amdgcn_exp2f(ml[0] - m);
-    l = __builtin_fmaf(f, ml[1], l);
-    const f32x4 u = *reinterpret_cast<const f32x4 *>(p.part_rows + at * D + c),
-                v = *reinterpret_cast<const f32x4 *>(p.part_rows + at * D + c + 4);
+    for (int s = group; s < p.parts; s += GROUPS) {
+      const size_t at = (size_t)(s * total + row);
+      const f32x2 ml = *reinterpret_cast<const f32x2 *>(p.part_ml + 2 * at);
+      if (ml[1] == 0.f) continue;
+      const float f = __builtin_amdgcn_exp2f(ml[0] - m);
+      l = __builtin_fmaf(f, ml[1], l);
+      const f32x4 u = *reinterpret_cast<const f32x4 *>(p.part_rows + at * D + c),
+                  v = *reinterpret_cast<const f32x4 *>(p.part_rows + at * D + c + 4);
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      x[j] = __builtin_fmaf(f, u[j], x[j]);
-      x[4 + j] = __builtin_fmaf(f, v[j], x[4 + j]);
+      for (int j = 0; j < 4; ++j) {
+        x[j] = __builtin_fmaf(f, u[j], x[j]);
+        x[4 + j] = __builtin_fmaf(f, v[j], x[4 + j]);
+      }
     }
   }
+  if constexpr (GROUPS > 1) {  // the groups' sums, in their order
+#pragma unroll
+    for (int j = 0; j < 8; ++j) sums[group][in_wg * D + c + j] = x[j];
+    if (c == 0) shares[group][in_wg] = l;
+    __syncthreads();
+    if (group > 0) return;
+#pragma unroll
+    for (int g = 1; g < GROUPS; ++g) {
+      l += shares[g][in_wg];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) x[j] += sums[g][in_wg * D + c + j];
+    }
+  }
+  if (!there) return;
   const float inv = l == 0.f ? 0.f : 1.0f / l;
   u32x4 w;
 #pragma unroll

@@ -196,9 +196,10 @@ __global__ __launch_bounds__(256, 2) void window_attn_dq_kernel(
   constexpr int BQ = Tile::BLOCK, DS = Tile::DS, DB = Tile::DB, AHEAD = Tile::AHEAD, RA = Tile::RA;
   extern __shared__ __attribute__((aligned(1024))) char lds[];
   const int nbq = (p.Nq + BQ - 1) / BQ;
-  const int unit = window_unit(p.B * p.Hq * nbq);
+  const int unit = window_unit(p.B * p.Hq * nbq * p.dq_parts);
   if (unit < 0) return;
-  const int bh = unit / nbq, r = nbq - 1 - (unit - bh * nbq), b = bh / p.Hq, h = bh - b * p.Hq;
+  const int part = unit % p.dq_parts, of_q = unit / p.dq_parts;
+  const int bh = of_q / nbq, r = nbq - 1 - (of_q - bh * nbq), b = bh / p.Hq, h = bh - b * p.Hq;
   const WindowEntry e(p, b);
   const Tile w(lds);
   const int i0 = r * BQ, i1 = min(i0 + BQ, e.q_len), col = i0 + w.wave * Tile::COLS + w.l32;
@@ -210,13 +211,15 @@ __global__ __launch_bounds__(256, 2) void window_attn_dq_kernel(
     for (int v = 0; v < 16; ++v) dq[db][v] = 0.f;
   if (i0 < i1) {
     const Tiles tiles(p, e, i0, i1);
+    // tiles [t0, t0 + n) of the block, counted from 0 below
+    const int t0 = (int)((long long)tiles.n * part / p.dq_parts), n_tiles = (int)((long long)tiles.n * (part + 1) / p.dq_parts) - t0;
     const size_t kv_head = (size_t)b * p.kv.b + (size_t)(h / (p.Hq / p.Hkv)) * p.kv.h;
     const uint32_t row_bytes = (uint32_t)p.kv.n * 2;
     u32x4 Kres = head_rsrc(gk + kv_head, 0), Vres = head_rsrc(gv + kv_head, 0);
     auto issue = [&](int t) {  // a tile behind the last one reads nothing
-      const int end = t < tiles.n ? tiles.end(t) : 0;
+      const int end = t < n_tiles ? tiles.end(t0 + t) : 0;
       Kres[2] = Vres[2] = __builtin_amdgcn_readfirstlane(end > 0 ? (uint32_t)(end - 1) * row_bytes + Tile::ROWB : 0u);
-      const int first = __builtin_amdgcn_readfirstlane(t < tiles.n ? tiles.row(t) : 0);
+      const int first = __builtin_amdgcn_readfirstlane(t < n_tiles ? tiles.row(t0 + t) : 0);
       w.issue(Kres, Vres, first, (uint32_t)(t & 3) * Tile::PAIR, row_bytes, row_bytes);
     };
     issue(0);
@@ -246,7 +249,7 @@ __global__ __launch_bounds__(256, 2) void window_attn_dq_kernel(
         }
       dl = sum_with_other_half(dl);
       dl *= Tile::DS_OF_P;
-      if (w.g == 0 && col < i1) {  // for dK and dV: [head][lse2, delta][query]
+      if (w.g == 0 && col < i1 && part == 0) {  // for dK and dV: [head][lse2, delta][query]
         stats[2 * row0 + col] = lse2;
         stats[2 * row0 + p.Nq + col] = dl;
       }
@@ -269,7 +272,7 @@ __global__ __launch_bounds__(256, 2) void window_attn_dq_kernel(
       mfma_gap<T, true, k == 0>(s, a[0], q[k]);
     });
     static_unroll<AHEAD>([&](auto i) { a[i] = Tile::rows_of(before.rows, Tile::TILE, i); });
-    for (int t = 0; t < tiles.n; ++t) {
+    for (int t = 0; t < n_tiles; ++t) {
       // dP, dQ of tile t - 1, S of tile t + 1; exponentials and dS beside the first two
       const typename Tile::Places at = place_of(t), next = place_of(t + 1);
       constexpr int N = 3 * DS;
@@ -294,11 +297,11 @@ __global__ __launch_bounds__(256, 2) void window_attn_dq_kernel(
         else mfma_gap<T, true, g == 2 * DS>(s, a[g % RA], q[g - 2 * DS]);
         if constexpr (g == 0) {
           settle<true>(s);
-          if (!tiles.whole(t)) {  // the keys that a query does not see: a probability of 2^-inf
+          if (!tiles.whole(t0 + t)) {  // the keys that a query does not see: a probability of 2^-inf
             int from, end;
-            tile_interval(tiles, t, lo, hi, from, end);
+            tile_interval(tiles, t0 + t, lo, hi, from, end);
             const uint32_t span = (uint32_t)max(end - from, 0);
-            from = tiles.row(t) + 8 * w.g - from;
+            from = tiles.row(t0 + t) + 8 * w.g - from;
 #pragma unroll
             for (int v = 0; v < 16; ++v) s[v] = (uint32_t)(from + 16 * (v >> 3) + (v & 7)) < span ? s[v] : unseen;
           }
@@ -320,7 +323,7 @@ __global__ __launch_bounds__(256, 2) void window_attn_dq_kernel(
       ds_before[1] = ds[1];
     }
     settle<true>(s);  // nothing reads the last S, but its registers are written again
-    if (tiles.n > 0)
+    if (n_tiles > 0)
       static_unroll<DS>([&](auto k) {
         a[0] = Tile::cols_of(before.cols, 0, k / DB, k % DB);
         mfma_gap<T, false, false>(dq[k % DB], a[0], ds_before[k / DB]);
@@ -329,8 +332,17 @@ __global__ __launch_bounds__(256, 2) void window_attn_dq_kernel(
 #pragma unroll
     for (int db = 0; db < DB; ++db) settle<false>(dq[db]);
   }
-  if (col < p.Nq)
+  if (col >= p.Nq) return;
+  if (p.dq_parts > 1) {
+    float *const to = p.part_dq + ((size_t)part * ((size_t)p.B * p.Hq * p.Nq) + row0 + col) * D + 4 * w.g;
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+#pragma unroll
+      for (int a = 0; a < 4; ++a)
+        *reinterpret_cast<f32x4 *>(to + 32 * db + 8 * a) = f32x4{dq[db][4 * a], dq[db][4 * a + 1], dq[db][4 * a + 2], dq[db][4 * a + 3]};
+  } else {
     Tile::store(dq, p.scale / GradScale<T>::DS, col < i1, gdq + (size_t)b * p.dq.b + (size_t)h * p.dq.h + (size_t)col * p.dq.n, w.g);
+  }
 }
 
 // ---- dK, dV -------------------------------------------------------------------------------------------------
@@ -585,41 +597,60 @@ __global__ __launch_bounds__(512, 2) void window_attn_dkv_kernel(
   Tile::store(dv, Tile::P_UNIT, there, gdv + at, w.g);
 }
 
-// Sums of the parts of every key's row, in the order of the parts, rounded once.
+// Sums of the parts of every key's row, and behind them of every query's, in the order of the parts, rounded once.
 template <int D, typename T>
-__global__ __launch_bounds__(256) void window_attn_dkv_sum_kernel(uint16_t *__restrict__ gdk, uint16_t *__restrict__ gdv,
-                                                                  const WindowDims p) {
+__global__ __launch_bounds__(256) void window_attn_grad_sum_kernel(uint16_t *__restrict__ gdq, uint16_t *__restrict__ gdk,
+                                                                   uint16_t *__restrict__ gdv, const WindowDims p) {
   using Tile = DkvTile<D, T>;
   constexpr int LANES = D / 8, BKV = Tile::BLOCK;
   const size_t rows = (size_t)p.B * p.Hkv * p.Nk;
   // with whole blocks beside those with sinks, only the rows of the latter are left to be added up
-  const int cut = p.bwd_parts > 1 ? p.Nk : min(p.Nk, p.n_sink_blocks * BKV);
-  const long long item = (long long)blockIdx.x * (256 / LANES) + threadIdx.x / LANES;
-  if (item >= 2ll * p.B * p.Hkv * cut) return;
-  const int which = (int)(item & 1), key = (int)((item >> 1) % cut), bh = (int)((item >> 1) / cut);
-  const bool sink = key < p.n_sink_blocks * BKV;
-  const size_t n = sink ? (size_t)p.B * p.Hkv * p.n_sink_blocks * BKV : rows;
-  const size_t first = sink && p.bwd_parts > 1 ? (size_t)p.bwd_parts * 2 * rows : 0;
-  const size_t row = sink ? (size_t)bh * p.n_sink_blocks * BKV + key : (size_t)bh * p.Nk + key;
-  const int parts = sink ? p.bwd_sink_parts : p.bwd_parts, c = 8 * (threadIdx.x % LANES);
-  const float *from = p.part_dkv + (first + which * n + row) * D + c;
+  const int cut = p.bwd_parts > 1 ? p.Nk : p.bwd_sink_parts > 1 ? min(p.Nk, p.n_sink_blocks * BKV) : 0;
+  const long long item = (long long)blockIdx.x * (256 / LANES) + threadIdx.x / LANES, of_keys = 2ll * p.B * p.Hkv * cut;
+  const int c = 8 * (threadIdx.x % LANES);
+  const float *from;
+  size_t step;
+  int parts, b;
+  uint16_t *to;
+  float f = p.scale / GradScale<T>::DS;
+  bool there;
+  if (item < of_keys) {
+    const int which = (int)(item & 1), key = (int)((item >> 1) % cut), bh = (int)((item >> 1) / cut), hk = bh % p.Hkv;
+    const bool sink = key < p.n_sink_blocks * BKV;
+    const size_t n = sink ? (size_t)p.B * p.Hkv * p.n_sink_blocks * BKV : rows;
+    const size_t first = sink && p.bwd_parts > 1 ? (size_t)p.bwd_parts * 2 * rows : 0;
+    const size_t row = sink ? (size_t)bh * p.n_sink_blocks * BKV + key : (size_t)bh * p.Nk + key;
+    from = p.part_dkv + (first + which * n + row) * D;
+    step = 2 * n * D;
+    parts = sink ? p.bwd_sink_parts : p.bwd_parts;
+    b = bh / p.Hkv;
+    to = (which ? gdv : gdk) + (size_t)b * p.dkv.b + (size_t)hk * p.dkv.h + (size_t)key * p.dkv.n;
+    if (which) f = Tile::P_UNIT;
+    there = key < (p.k_len ? min(p.k_len[b], p.Nk) : p.Nk);
+  } else {
+    const long long row = item - of_keys, n = (long long)p.B * p.Hq * p.Nq;
+    if (p.dq_parts == 1 || row >= n) return;
+    const int i = (int)(row % p.Nq), bh = (int)(row / p.Nq);
+    from = p.part_dq + (size_t)row * D;
+    step = (size_t)n * D;
+    parts = p.dq_parts;
+    b = bh / p.Hq;
+    to = gdq + (size_t)b * p.dq.b + (size_t)(bh % p.Hq) * p.dq.h + (size_t)i * p.dq.n;
+    there = i < (p.q_len ? min(p.q_len[b], p.Nq) : p.Nq);
+  }
   float x[8];
 #pragma unroll
   for (int j = 0; j < 8; ++j) x[j] = 0.f;
 #pragma unroll 4
-  for (int s = 0; s < parts; ++s, from += 2 * n * D) {
-    const f32x4 u = *reinterpret_cast<const f32x4 *>(from), v = *reinterpret_cast<const f32x4 *>(from + 4);
+  for (int s = 0; s < parts; ++s, from += step) {
+    const f32x4 u = *reinterpret_cast<const f32x4 *>(from + c), v = *reinterpret_cast<const f32x4 *>(from + c + 4);
 #pragma unroll
     for (int j = 0; j < 4; ++j) x[j] += u[j], x[4 + j] += v[j];
   }
-  const int b = bh / p.Hkv, hk = bh - b * p.Hkv;
-  const WindowEntry e(p, b);
-  const float f = which ? Tile::P_UNIT : p.scale / GradScale<T>::DS;
   u32x4 out;
 #pragma unroll
-  for (int j = 0; j < 4; ++j) out[j] = key < e.k_len ? T::pack(x[2 * j] * f, x[2 * j + 1] * f) : 0u;
-  uint16_t *const to = which ? gdv : gdk;
-  *reinterpret_cast<u32x4 *>(to + (size_t)b * p.dkv.b + (size_t)hk * p.dkv.h + (size_t)key * p.dkv.n + c) = out;
+  for (int j = 0; j < 4; ++j) out[j] = there ? T::pack(x[2 * j] * f, x[2 * j + 1] * f) : 0u;
+  *reinterpret_cast<u32x4 *>(to + c) = out;
 }
 
 }  // namespace calibatt_dev

@@ -368,12 +368,13 @@ __global__ __launch_bounds__(256) void layer_norm_fwd_kernel(const typename T::t
 }
 
 // Gradients.  A workgroup goes over the rows with steps of the grid and keeps its share of dw and db in registers; at
-// the end it leaves them as row blockIdx.x of `partial` ([gridDim.x][2][C], NULL without weights), which
-// layer_norm_params_kernel adds up: a fixed order of additions, no atomics.
+// the end it leaves them as row blockIdx.x of `partial` ([gridDim.x][2][C]), which layer_norm_params_kernel adds up: a
+// fixed order of additions, no atomics.  A single workgroup's shares are the sums, and go to gdw and gdb (NULL: not
+// asked for).
 template <typename T, int VEC, int LPR, int NV>
 __global__ __launch_bounds__(256) void layer_norm_bwd_kernel(const typename T::type *__restrict__ dy, const typename T::type *__restrict__ x,
                                                              const void *__restrict__ weight, typename T::type *__restrict__ dx,
-                                                             float *__restrict__ partial, const NormDims p) {
+                                                             float *__restrict__ partial, void *gdw, void *gdb, const NormDims p) {
   using Row = NormRow<T, VEC, LPR, NV>;
   constexpr int EL = NV * VEC;
   __shared__ float red[24];
@@ -444,15 +445,20 @@ __global__ __launch_bounds__(256) void layer_norm_bwd_kernel(const typename T::t
       if (r.column(v) < p.C) Row::store(out + r.column(v), g + v * VEC);
     }
   }
-  if (!partial) return;
-  float *const mine = partial + (size_t)blockIdx.x * 2 * p.C;
-  auto leave = [&](const float (&share)[EL], float *to) {
+  if (!gdw && !gdb) return;
+  const bool alone = gridDim.x == 1;
+  auto put = [&](void *sums, int which, int c, float s) {
+    if (!alone) partial[((size_t)blockIdx.x * 2 + which) * p.C + c] = s;
+    else if (sums && p.weight_f32) ((float *)sums)[c] = s;
+    else if (sums) ((typename T::type *)sums)[c] = T::put(s);
+  };
+  auto leave = [&](const float (&share)[EL], void *sums, int which) {
     if constexpr (Row::GROUPS == 1) {
 #pragma unroll
       for (int v = 0; v < NV; ++v)
 #pragma unroll
         for (int e = 0; e < VEC; ++e)
-          if (r.column(v) + e < p.C) to[r.column(v) + e] = share[v * VEC + e];
+          if (r.column(v) + e < p.C) put(sums, which, r.column(v) + e, share[v * VEC + e]);
     } else {
       constexpr int W = LPR * EL;
       __syncthreads();
@@ -465,12 +471,12 @@ __global__ __launch_bounds__(256) void layer_norm_bwd_kernel(const typename T::t
         float s = 0.f;
 #pragma unroll
         for (int i = 0; i < Row::GROUPS; ++i) s += shares[i * W + c];
-        to[c] = s;
+        put(sums, which, c, s);
       }
     }
   };
-  leave(dw, mine);
-  leave(db, mine + p.C);
+  leave(dw, gdw, 0);
+  leave(db, gdb, 1);
 }
 
 // Columns of `partial` ([n][2][C]) added up: COLS columns per workgroup, its 256 / COLS slices of the n rows one after

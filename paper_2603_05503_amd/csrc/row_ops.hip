@@ -152,6 +152,9 @@ bool norm_tensor_ok(const void *ptr, const calibatt_strides &s, int bytes) {
 // and db that is written and read again, so more of them cost more (5120 columns, 32 760 rows: 21 MB of shares beside
 // 1 007 MB); fewer keep too few rows in flight.
 constexpr int NORM_BWD_WGS_PER_CU = 2;
+// Rounds of rows that one workgroup takes by itself, and adds up without a second launch (16 rows of 88: 17 us with one,
+// @NORMALONE@ without).
+constexpr int NORM_BWD_ALONE = 8;
 
 template <typename T>
 int launch_norm_fwd(const NormTensors &t, const void *weight, const void *bias, bool wide, const NormDims &p, hipStream_t stream) {
@@ -175,11 +178,12 @@ int launch_norm_bwd(const NormTensors &t, const void *weight, bool wide, const N
     constexpr int GROUPS = 256 / lpr;
     constexpr int SMEM = GROUPS == 1 ? 0 : 256 * vec * nv * 4;
     grid = std::min((p.rows + GROUPS - 1) / GROUPS, cus * NORM_BWD_WGS_PER_CU);
+    if (grid <= NORM_BWD_ALONE) grid = 1;
     typedef typename T::type E;
     return launch_kernel(layer_norm_bwd_kernel<T, vec, lpr, nv>, (unsigned)grid, 256, SMEM, stream, (const E *)t.dy,
-                         (const E *)t.x, weight, (E *)t.y, partial, p);
+                         (const E *)t.x, weight, (E *)t.y, partial, dweight, dbias, p);
   });
-  if (st != CALIBATT_OK || !partial) return st;
+  if (st != CALIBATT_OK || grid == 1 || !(dweight || dbias)) return st;
   // few columns: narrow pieces of them, so that many lanes share the rows of each
   if (p.C <= 512)
     return launch_kernel(layer_norm_params_kernel<T, 8>, (unsigned)((2 * p.C + 7) / 8), 256, 0, stream, (const float *)partial,

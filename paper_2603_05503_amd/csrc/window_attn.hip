@@ -34,7 +34,7 @@ bool is_step(int Hq, int Hkv, int Nq) { return (int64_t)(Hq / Hkv) * Nq <= 32; }
 int forward_parts(int B, int Hq, int Hkv, int Nq, int Nk, const calibatt_window &w) {
   if (is_step(Hq, Hkv, Nq)) {
     const int64_t units = (int64_t)B * Hkv, tiles = window_tiles(w, Nq, Nk, STEP_KEYS);
-    if (tiles <= 4 * STEP_WAVES) return 1;  // a second launch costs more than the four rounds of the waves
+    if (tiles <= 8 * STEP_WAVES) return 1;  // a second launch costs more than eight rounds of the waves
     const int64_t fill = std::max<int64_t>(1, 2 * WINDOW_CUS / units);
     return (int)std::max<int64_t>(1, std::min<int64_t>({fill, (tiles + 2 * STEP_WAVES - 1) / (2 * STEP_WAVES), WINDOW_MAX_PARTS}));
   }
@@ -109,15 +109,18 @@ int launch_forward(const uint16_t *q, const uint16_t *k, const uint16_t *v, uint
     st = launch_kernel(window_attn_fwd_kernel<D, T>, grid, 256, SMEM, stream, q, k, v, out, lse, p);
   }
   if (st || p.parts == 1) return st;
-  const int64_t rows = (int64_t)p.B * p.Hq * p.Nq, per_wg = 256 / (D / 8);
-  return launch_kernel(window_attn_merge_kernel<D, T>, (unsigned)((rows + per_wg - 1) / per_wg), 256, 0, stream, out, lse, p);
+  const int64_t rows = (int64_t)p.B * p.Hq * p.Nq;
+  constexpr int PER_WG = 256 / (D / 8);
+  if (rows <= 2 * WINDOW_CUS)
+    return launch_kernel(window_attn_merge_kernel<D, 1, T>, (unsigned)rows, 256, 0, stream, out, lse, p);
+  return launch_kernel(window_attn_merge_kernel<D, PER_WG, T>, (unsigned)((rows + PER_WG - 1) / PER_WG), 256, 0, stream, out, lse, p);
 }
 
 // ---- gradients ----------------------------------------------------------------------------------------------
 // How the queries that see a block of 256 keys are cut into parts.  A block with sinks is seen by all later queries, so it
 // gets parts as long as the others'.
 struct GradPlan {
-  int parts, sink_parts, sink_blocks;
+  int dq_parts, parts, sink_parts, sink_blocks;
   int64_t bytes;  // of the workspace: lse and delta of every query, and the sums of the parts
 };
 GradPlan grad_plan(int B, int Hq, int Hkv, int Nq, int Nk, int D, const calibatt_window &w) {
@@ -144,7 +147,10 @@ GradPlan grad_plan(int B, int Hq, int Hkv, int Nq, int Nk, int D, const calibatt
     g.parts = (int)parts;
     g.sink_parts = (int)std::max<int64_t>(1, sink_parts);
   }
-  g.bytes = ((int64_t)B * Hq * Nq + 1) / 2 * 16;
+  // dQ: of a few blocks of queries the tiles of keys are cut, to a dozen at least
+  const int64_t q_rows = (int64_t)B * Hq * Nq, q_units = (int64_t)B * Hq * ((Nq + 127) / 128);
+  g.dq_parts = (int)std::max<int64_t>(1, std::min<int64_t>({2 * WINDOW_CUS / q_units, window_tiles(w, 128, Nk, ROWS) / 12, WINDOW_MAX_PARTS}));
+  g.bytes = (q_rows + 1) / 2 * 16 + (g.dq_parts > 1 ? g.dq_parts * q_rows * D * 4 : 0);
   const int64_t row = 2 * D * 4;
   if (g.parts > 1) g.bytes += g.parts * heads * Nk * row;
   if (g.sink_blocks && g.sink_parts > 1) g.bytes += g.sink_parts * heads * g.sink_blocks * BLOCK * row;
@@ -165,10 +171,11 @@ int launch_backward(const GradTensors &t, const WindowDims &p, hipStream_t strea
   int unused = 0;
   if (int st = prepare(window_attn_dq_kernel<D, T>, 256, DQ_LDS, dq_info, unused)) return st;
   if (int st = prepare(window_attn_dkv_kernel<D, T>, 512, DKV_LDS, dkv_info, unused)) return st;
-  const int64_t q_units = (int64_t)p.B * p.Hq * ((p.Nq + BLOCK_Q - 1) / BLOCK_Q), blocks = (p.Nk + BLOCK - 1) / BLOCK;
+  const int64_t q_units = (int64_t)p.B * p.Hq * ((p.Nq + BLOCK_Q - 1) / BLOCK_Q) * p.dq_parts, blocks = (p.Nk + BLOCK - 1) / BLOCK;
   const int64_t k_units = (int64_t)p.B * p.Hkv * (p.n_sink_blocks * p.bwd_sink_parts + (blocks - p.n_sink_blocks) * p.bwd_parts);
   const int64_t cut = p.bwd_parts > 1 ? p.Nk : p.bwd_sink_parts > 1 ? std::min(p.Nk, p.n_sink_blocks * BLOCK) : 0;
-  const int64_t per_wg = 256 / (D / 8), sum_wgs = (2 * cut * p.B * p.Hkv + per_wg - 1) / per_wg;
+  const int64_t sums = 2 * cut * p.B * p.Hkv + (p.dq_parts > 1 ? (int64_t)p.B * p.Hq * p.Nq : 0);
+  const int64_t per_wg = 256 / (D / 8), sum_wgs = (sums + per_wg - 1) / per_wg;
   if (q_units > 0x7ffffff0LL || k_units > 0x7ffffff0LL || sum_wgs > 0x7fffffffLL) return CALIBATT_ERR_SHAPE;
   if (int st = launch_kernel(window_attn_dq_kernel<D, T>, (unsigned)(8 * ((q_units + 7) / 8)), 256, DQ_LDS, stream, t.dout, t.q, t.k,
                              t.v, t.out, t.lse, t.dq, t.stats, p))
@@ -176,7 +183,7 @@ int launch_backward(const GradTensors &t, const WindowDims &p, hipStream_t strea
   if (int st = launch_kernel(window_attn_dkv_kernel<D, T>, (unsigned)(8 * ((k_units + 7) / 8)), 512, DKV_LDS, stream, t.dout, t.q,
                              t.k, t.v, (const float *)t.stats, t.dk, t.dv, p))
     return st;
-  return sum_wgs ? launch_kernel(window_attn_dkv_sum_kernel<D, T>, (unsigned)sum_wgs, 256, 0, stream, t.dk, t.dv, p) : CALIBATT_OK;
+  return sum_wgs ? launch_kernel(window_attn_grad_sum_kernel<D, T>, (unsigned)sum_wgs, 256, 0, stream, t.dq, t.dk, t.dv, p) : CALIBATT_OK;
 }
 
 }  // namespace
@@ -249,10 +256,12 @@ extern "C" int calibatt_window_attn_bwd(const void *dout, const void *q, const v
   if ((at & 15) || ((uintptr_t)lse & 3)) return CALIBATT_ERR_SHAPE;
   const GradPlan g = grad_plan(B, Hq, Hkv, Nq, Nk, D, *window);
   if (workspace_bytes < g.bytes) return CALIBATT_ERR_BUFFER_TOO_SMALL;
+  p.dq_parts = g.dq_parts;
   p.bwd_parts = g.parts;
   p.bwd_sink_parts = g.sink_parts;
   p.n_sink_blocks = g.sink_blocks;
-  p.part_dkv = (float *)workspace + ((int64_t)B * Hq * Nq + 1) / 2 * 4;
+  p.part_dq = (float *)workspace + ((int64_t)B * Hq * Nq + 1) / 2 * 4;
+  p.part_dkv = p.part_dq + (g.dq_parts > 1 ? (int64_t)g.dq_parts * B * Hq * Nq * D : 0);
   const GradTensors t = {(const uint16_t *)dout, (const uint16_t *)q, (const uint16_t *)k, (const uint16_t *)v,
                          (const uint16_t *)out, lse, (uint16_t *)dq, (uint16_t *)dk, (uint16_t *)dv, (float *)workspace};
   hipStream_t s = (hipStream_t)stream;
