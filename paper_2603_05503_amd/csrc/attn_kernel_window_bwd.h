@@ -16,7 +16,7 @@
 // barrier; the second wave of the SIMD fills what one leaves.  Us of dQ, and of dK and dV, for 16 380 tokens, 8 query heads
 // on 4 key heads, D = 128, nine frames of 780 and the first: scheduled by the compiler, 64 columns to a wave, one wave per
 // SIMD 930 and 2660 (it gathers reads and vector work and spills), the same in gaps 787 and 1253 (half its cycles waits),
-// this form @GAPS@.
+// this form 655 and 990.
 #pragma once
 #include "attn_kernel_window.h"
 
@@ -199,7 +199,10 @@ __global__ __launch_bounds__(256, 2) void window_attn_dq_kernel(
   const int unit = window_unit(p.B * p.Hq * nbq * p.dq_parts);
   if (unit < 0) return;
   const int part = unit % p.dq_parts, of_q = unit / p.dq_parts;
-  const int bh = of_q / nbq, r = nbq - 1 - (of_q - bh * nbq), b = bh / p.Hq, h = bh - b * p.Hq;
+  const int x = of_q / nbq, r = nbq - 1 - (of_q - x * nbq);
+  int b, h;
+  window_head(x, p.B, p.Hq / p.Hkv, b, h);
+  const int bh = b * p.Hq + h;
   const WindowEntry e(p, b);
   const Tile w(lds);
   const int i0 = r * BQ, i1 = min(i0 + BQ, e.q_len), col = i0 + w.wave * Tile::COLS + w.l32;
@@ -403,8 +406,10 @@ __global__ __launch_bounds__(512, 2) void window_attn_dkv_kernel(
   const int nkb = (p.Nk + BKV - 1) / BKV, per_head = grad_units(p, nkb);
   const int unit = window_unit(p.B * p.Hkv * per_head);
   if (unit < 0) return;
-  const int bh = unit / per_head, b = bh / p.Hkv, hk = bh - b * p.Hkv;
-  int rest = unit - bh * per_head, block, part, parts;
+  const int x = unit / per_head;
+  int b, hk, rest = unit - x * per_head, block, part, parts;
+  window_head(x, p.B, 1, b, hk);
+  const int bh = b * p.Hkv + hk;
   const bool sink_block = rest < p.n_sink_blocks * p.bwd_sink_parts;
   if (sink_block) {
     parts = p.bwd_sink_parts;

@@ -31,7 +31,12 @@ int device_cus(int &cus) {
 }
 
 // ---- rotary positions ---------------------------------------------------------------------------------------
-bool rope_strides_ok(const calibatt_strides &s, int D) {
+// Strides of a tensor; those of an axis of one entry are never stepped along.
+bool rope_strides(const calibatt_strides *given, int B, int H, int N, int D, Strides &s) {
+  s = given ? Strides{given->b, given->h, given->n} : Strides{(int64_t)H * N * D, (int64_t)N * D, D};
+  if (B == 1) s.b = 0;
+  if (H == 1) s.h = 0;
+  if (N == 1) s.n = D;
   return s.n >= D && s.b >= 0 && s.h >= 0 && s.n % 8 == 0 && s.h % 8 == 0 && s.b % 8 == 0;
 }
 
@@ -153,7 +158,7 @@ bool norm_tensor_ok(const void *ptr, const calibatt_strides &s, int bytes) {
 // 1 007 MB); fewer keep too few rows in flight.
 constexpr int NORM_BWD_WGS_PER_CU = 2;
 // Rounds of rows that one workgroup takes by itself, and adds up without a second launch (16 rows of 88: 17 us with one,
-// @NORMALONE@ without).
+// 14 without).
 constexpr int NORM_BWD_ALONE = 8;
 
 template <typename T>
@@ -258,15 +263,13 @@ extern "C" int calibatt_rope_axes(const void *q, void *q_out, const void *k, voi
     }
     p.n_grid = (int)n_grid;
   }
-  const calibatt_strides packed_q = {(int64_t)Hq * N * D, (int64_t)N * D, D}, packed_k = {(int64_t)Hk * N * D, (int64_t)N * D, D};
-  const calibatt_strides *const s[4] = {q_strides ? q_strides : &packed_q, q_out_strides ? q_out_strides : &packed_q,
-                                        k_strides ? k_strides : &packed_k, k_out_strides ? k_out_strides : &packed_k};
+  const calibatt_strides *const given[4] = {q_strides, q_out_strides, k_strides, k_out_strides};
+  Strides s[4] = {};
   for (int i = 0; i < (k ? 4 : 2); ++i)
-    if (!rope_strides_ok(*s[i], D)) return CALIBATT_ERR_SHAPE;
+    if (!rope_strides(given[i], B, i < 2 ? Hq : Hk, N, D, s[i])) return CALIBATT_ERR_SHAPE;
   if (((uintptr_t)q | (uintptr_t)q_out | (uintptr_t)k | (uintptr_t)(k ? k_out : nullptr)) & 15) return CALIBATT_ERR_SHAPE;
   if ((uintptr_t)rope->table & 7) return CALIBATT_ERR_SHAPE;
-  auto dev = [](const calibatt_strides &x) { return Strides{x.b, x.h, x.n}; };
-  const RopeTensor tq = {q, q_out, dev(*s[0]), dev(*s[1]), Hq}, tk = {k, k_out, dev(*s[2]), dev(*s[3]), Hk};
+  const RopeTensor tq = {q, q_out, s[0], s[1], Hq}, tk = {k, k_out, s[2], s[3], Hk};
   p.units = halves ? p.pairs / 8 + (D - 2 * p.pairs) / 8 : D / 8;
   p.tokens_per_wg = 256 / p.units;
   // Heads of one workgroup: as many as leave every CU eight workgroups, at most 16 (the tables are then read for one
@@ -303,7 +306,7 @@ extern "C" int calibatt_layer_norm_fwd(const void *x, const void *weight, const 
   const calibatt_strides *const s[3] = {&sx, &sx, &sy};
   NormDims p;
   if (int st = norm_dims(n, s, C, eps, center, weight_dtype == CALIBATT_F32, p)) return st;
-  const bool wide = norm_wide(x, sx, C, bytes) && norm_wide(y, sy, C, bytes);
+  const bool wide = norm_wide(x, sx, C, bytes) && norm_wide(y, sy, C, bytes) && (((uintptr_t)weight | (uintptr_t)bias) & 15) == 0;
   const NormTensors t = {x, nullptr, y};
   hipStream_t hs = (hipStream_t)stream;
   return dtype == CALIBATT_BF16  ? launch_norm_fwd<RowBf16>(t, weight, bias, wide, p, hs)
@@ -345,7 +348,8 @@ extern "C" int calibatt_layer_norm_bwd(const void *dy, const void *x, const void
   const calibatt_strides *const s[3] = {&sx, &sg, &sd};
   NormDims p;
   if (int st = norm_dims(n, s, C, eps, center, weight_dtype == CALIBATT_F32, p)) return st;
-  const bool wide = norm_wide(x, sx, C, bytes) && norm_wide(dy, sg, C, bytes) && norm_wide(dx, sd, C, bytes);
+  const bool wide = norm_wide(x, sx, C, bytes) && norm_wide(dy, sg, C, bytes) && norm_wide(dx, sd, C, bytes) &&
+                    (((uintptr_t)weight | (uintptr_t)workspace) & 15) == 0;
   const NormTensors t = {x, dy, dx};
   hipStream_t hs = (hipStream_t)stream;
   float *const partial = params ? workspace : nullptr;

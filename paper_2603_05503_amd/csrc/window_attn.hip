@@ -39,8 +39,10 @@ int forward_parts(int B, int Hq, int Hkv, int Nq, int Nk, const calibatt_window 
     return (int)std::max<int64_t>(1, std::min<int64_t>({fill, (tiles + 2 * STEP_WAVES - 1) / (2 * STEP_WAVES), WINDOW_MAX_PARTS}));
   }
   const int64_t units = (int64_t)B * Hq * ((Nq + 127) / 128), tiles = window_tiles(w, 128, Nk, 64);
+  // As many as fill the GPU, of eight tiles at least: 4 heads of 3000 tokens, all keys, 56 us whole, 40 in four parts; 8 heads
+  // of 875, three frames of 134, D = 64, 19 whole, 22 in two.
   const int64_t fill = 2 * WINDOW_CUS / units;
-  return (int)std::max<int64_t>(1, std::min<int64_t>({fill, tiles / 6, WINDOW_MAX_PARTS}));
+  return (int)std::max<int64_t>(1, std::min<int64_t>({fill, tiles / 8, WINDOW_MAX_PARTS}));
 }
 
 int64_t forward_bytes(int parts, int B, int Hq, int Nq, int D) {
@@ -132,7 +134,9 @@ GradPlan grad_plan(int B, int Hq, int Hkv, int Nq, int Nk, int D, const calibatt
   int64_t one = all;  // tiles of queries that see a block, without sinks
   if (w.left >= 0 && w.right >= 0) one = std::min<int64_t>(all, G * ((window_span(w, BLOCK, Nq) + ROWS - 1) / ROWS));
   // Rounds of workgroups times the length of a part, which costs so many tiles beside its own (its start, its sums to
-  // memory and back).
+  // memory and back).  All gradients, us, by parts: 8 heads on 4 of 16 380 tokens, nine frames of 780 and the first, 1 1900,
+  // 2 1696, 3 1615, 4 1616 (chosen), 8 1671; 8 on 2 of 5027, 870 keys, 1 268, 4 132, 6 124 (chosen), 8 153; 4 of 3000, all
+  // keys, 1 196, 4 109, 5 106 (chosen), 6 133; 40 of 1500 1 154 (chosen), 2 177.
   constexpr int64_t PART_COST = 12, ALONE = 4;
   double best = 0.0;
   g.parts = 0;
@@ -147,9 +151,10 @@ GradPlan grad_plan(int B, int Hq, int Hkv, int Nq, int Nk, int D, const calibatt
     g.parts = (int)parts;
     g.sink_parts = (int)std::max<int64_t>(1, sink_parts);
   }
-  // dQ: of a few blocks of queries the tiles of keys are cut, to a dozen at least
+  // dQ: of a few blocks of queries the tiles of keys are cut, to eight at least (all gradients of 6 heads of 1801 tokens, all
+  // keys so far: 107 us whole, 82 in four parts; 8 heads of 875, three frames of 134, D = 64: 51 and, in two, 45)
   const int64_t q_rows = (int64_t)B * Hq * Nq, q_units = (int64_t)B * Hq * ((Nq + 127) / 128);
-  g.dq_parts = (int)std::max<int64_t>(1, std::min<int64_t>({2 * WINDOW_CUS / q_units, window_tiles(w, 128, Nk, ROWS) / 12, WINDOW_MAX_PARTS}));
+  g.dq_parts = (int)std::max<int64_t>(1, std::min<int64_t>({2 * WINDOW_CUS / q_units, window_tiles(w, 128, Nk, ROWS) / 8, WINDOW_MAX_PARTS}));
   g.bytes = (q_rows + 1) / 2 * 16 + (g.dq_parts > 1 ? g.dq_parts * q_rows * D * 4 : 0);
   const int64_t row = 2 * D * 4;
   if (g.parts > 1) g.bytes += g.parts * heads * Nk * row;
