@@ -247,8 +247,9 @@ __device__ __forceinline__ float group_sum(float x) {
   return x;
 }
 
-// Sum over the LPR lanes of a row; with 256 lanes over the four waves through LDS, `slot` another one from sum to sum
-// (three in turn), so that one barrier per sum is enough.
+// Sum over the LPR lanes of a row; with 256 lanes over the four waves through LDS.  `slot` is never that of the sum before,
+// over the rows as well: a wave that is a sum ahead writes elsewhere than where others still read, and can't be two ahead,
+// as one barrier stands in every sum.
 template <int LPR>
 __device__ __forceinline__ void row_sums(float &a, float &b, float *red, int slot) {
   a = group_sum<LPR < 64 ? LPR : 64>(a);
@@ -332,6 +333,7 @@ __global__ __launch_bounds__(256) void layer_norm_fwd_kernel(const typename T::t
   }
   const float inv = 1.0f / p.C;
   typename Row::Raw next[NV];
+  int slot = 1;  // of the only sum that a row without a mean has: 1 and 2 in turn
   if (first < p.rows) r.load(x + norm_offset(p, p.x, first), p.C, next);
   for (int row = first; row < p.rows; row += step) {
     float xs[NV * VEC];
@@ -356,7 +358,8 @@ __global__ __launch_bounds__(256) void layer_norm_fwd_kernel(const typename T::t
         sq = __builtin_fmaf(d, d, sq);
       }
     }
-    row_sums<LPR>(sq, unused, red, 1);
+    row_sums<LPR>(sq, unused, red, slot);
+    slot ^= 3;
     const float rstd = 1.0f / sqrtf(__builtin_fmaf(sq, inv, p.eps));
     typename T::type *const out = y + norm_offset(p, p.y, row);
     if constexpr (VEC == 1) {  // too many columns for registers beside the row's, and cached

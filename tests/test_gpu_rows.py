@@ -224,6 +224,24 @@ def test_norm_and_gradients(lib, shape, dtype, wtype, center):
     assert lib.layer_norm_fwd(z, w, b, eps=eps, center=center, out=z) is z and torch.equal(z, y)
 
 
+@pytest.mark.parametrize("center", [True, False])
+@pytest.mark.parametrize("rows,C,dtype", [(6000, 2056, "bfloat16"), (6000, 301, "float32"), (4100, 5120, "float16")])
+def test_norm_of_many_long_rows(lib, rows, C, dtype, center):
+    """More rows of a workgroup each than workgroups: the sums of one row do not meet those of the next.  Rows of very
+    different size, so that a sum of the wrong row would show."""
+    torch = _torch()
+    rng = np.random.default_rng(rows)
+    gain = torch.from_numpy((2.0 ** rng.integers(-6, 7, (rows, 1))).astype(np.float32)).cuda()
+    x = (make(rng, (rows, C), "float32") * gain).to(getattr(torch, dtype))
+    y = lib.layer_norm_fwd(x, eps=1e-6, center=center)
+    xs = f64(x)
+    d = xs - xs.mean(-1, keepdims=True) if center else xs
+    r = 1 / np.sqrt((d * d).mean(-1, keepdims=True) + 1e-6)
+    assert_near(y, d * r, dtype, norm_slack(xs, 1.0, 0.0, d * r, r), "y")
+    for _ in range(3):
+        assert torch.equal(lib.layer_norm_fwd(x, eps=1e-6, center=center), y)
+
+
 @pytest.mark.parametrize("layout", ["bnhd", "fused"])
 @pytest.mark.parametrize("D", [64, 128, 40])
 def test_norm_of_heads_in_other_layouts(lib, layout, D):
