@@ -767,8 +767,8 @@ int calibatt_rope_axes(const void *q, void *q_out, const void *k, void *k_out, i
  * [C] NULL = zeros (a bias needs a weight); both of weight_dtype, which is dtype
  * or CALIBATT_F32.  Any strides >= 0 of b, h, n (NULL = packed); C contiguous.
  * Rows of whole, aligned 16-byte pieces take 16-byte accesses, others go element
- * by element.  y may be x with the same strides.  Statistics and arithmetic are
- * fp32, rounded once.
+ * by element.  y may be x with the same strides; its rows must not overlap.
+ * Statistics and arithmetic are fp32, rounded once.
  * Errors: NULL (also a bias without a weight); SHAPE (non-positive sizes, more
  * than 2^30 - 1 rows, eps negative or not a number, misaligned elements);
  * UNSUPPORTED (types, C above 8192); LAUNCH.
@@ -826,7 +826,8 @@ typedef struct calibatt_window {
  * needed): calls of few queries are cut along the keys and joined.  NULL: they
  * are not.  Calls that overlap on the GPU need workspaces of their own.
  * Strides as in calibatt_sparse_attn_fwd_strided (NULL = packed; k and v share
- * theirs); pointers 16-byte aligned.  Supported: D in {64, 128}.
+ * theirs; the rows of a head, and 256 more, within 2^32 bytes); pointers 16-byte
+ * aligned.  Supported: D in {64, 128}.
  * Errors: NULL; SHAPE (sizes not positive, Hq no multiple of Hkv, more than
  * 2^31 - 1 rows, a window with left or right below -1, sinks < 0, frame <= 0 or
  * |offset| > 2^30, strides, alignment, out an input, scale not finite);

@@ -81,7 +81,7 @@ struct RopeTensor {
   int H;
 };
 struct RopeDims {
-  int N, D, pairs, n_axes;
+  int N, pairs, n_axes;
   int end[ROPE_MAX_AXES];     // pairs of the axes so far
   int length[ROPE_MAX_AXES];  // positions that an axis's table has
   int at[ROPE_MAX_AXES];      // first entry of its table

@@ -31,9 +31,10 @@ int device_cus(int &cus) {
 }
 
 // ---- rotary positions ---------------------------------------------------------------------------------------
-// Strides of a tensor; those of an axis of one entry are never stepped along.
-bool rope_strides(const calibatt_strides *given, int B, int H, int N, int D, Strides &s) {
+// Strides of a tensor; those of an axis of one entry are never stepped along.  No two rows of an output may start in one.
+bool rope_strides(const calibatt_strides *given, int B, int H, int N, int D, bool output, Strides &s) {
   s = given ? Strides{given->b, given->h, given->n} : Strides{(int64_t)H * N * D, (int64_t)N * D, D};
+  if (output && ((B > 1 && s.b < D) || (H > 1 && s.h < D))) return false;
   if (B == 1) s.b = 0;
   if (H == 1) s.h = 0;
   if (N == 1) s.n = D;
@@ -68,8 +69,8 @@ struct NormTensors {
 
 // Rows in the order of memory, and as few indices as they need: the indices by falling distance in x, neighbours
 // joined where every tensor's distances allow it.
-int norm_dims(const int64_t n[3], const calibatt_strides *const s[3], int C, float eps, int center, int weight_f32,
-              NormDims &p) {
+void norm_dims(const int64_t n[3], const calibatt_strides *const s[3], int C, float eps, int center, int weight_f32,
+               NormDims &p) {
   struct Index {
     int64_t n, s[3];
   } list[3];
@@ -102,7 +103,6 @@ int norm_dims(const int64_t n[3], const calibatt_strides *const s[3], int C, flo
   p.eps = eps;
   p.center = center ? 1 : 0;
   p.weight_f32 = weight_f32;
-  return CALIBATT_OK;
 }
 
 // How a row of C elements lies in lanes: pieces of 16 bytes where they can be had, few lanes for short rows (several
@@ -149,8 +149,12 @@ int norm_check(int64_t B, int64_t H, int64_t N, int C, int dtype, int weight_dty
     return CALIBATT_ERR_UNSUPPORTED;
   return CALIBATT_OK;
 }
-bool norm_tensor_ok(const void *ptr, const calibatt_strides &s, int bytes) {
-  return ((uintptr_t)ptr & (bytes - 1)) == 0 && s.b >= 0 && s.h >= 0 && s.n >= 0;
+// `row`: elements that lie between two rows at least: C for an output, 0 for an input, whose rows may be one
+bool norm_tensor_ok(const void *ptr, const int64_t n[3], const calibatt_strides &s, int bytes, int row) {
+  const int64_t step[3] = {s.b, s.h, s.n};
+  for (int i = 0; i < 3; ++i)
+    if (step[i] < 0 || (n[i] > 1 && step[i] < row)) return false;
+  return ((uintptr_t)ptr & (bytes - 1)) == 0;
 }
 
 // Workgroups of the gradients' kernel at most, and rows of the workspace: two for every CU.  Each leaves a share of dw
@@ -229,12 +233,11 @@ extern "C" int calibatt_rope_axes(const void *q, void *q_out, const void *k, voi
   if (!q || !q_out || !rope || !rope->table || !place || (k && !k_out)) return CALIBATT_ERR_NULL;
   if (!k) Hk = 0;
   if (B <= 0 || Hq <= 0 || N <= 0 || D <= 0 || (k && Hk <= 0)) return CALIBATT_ERR_SHAPE;
-  if (B > 65535 || Hq > 0xffff || Hk > 0xffff) return CALIBATT_ERR_SHAPE;
+  if (B > 65535 || Hq > 0xffff || Hk > 0xffff || N > 1 << 30) return CALIBATT_ERR_SHAPE;
   if (!element_type_ok(dtype) || D % 8 || D > 1024) return CALIBATT_ERR_UNSUPPORTED;
   if (int st = rope_axes_ok(rope->n_axes, rope->dims, rope->length)) return st;
   RopeDims p = {};
   p.N = N;
-  p.D = D;
   p.n_axes = rope->n_axes;
   p.sign = inverse ? -1.f : 1.f;
   int at = 0;
@@ -266,12 +269,13 @@ extern "C" int calibatt_rope_axes(const void *q, void *q_out, const void *k, voi
   const calibatt_strides *const given[4] = {q_strides, q_out_strides, k_strides, k_out_strides};
   Strides s[4] = {};
   for (int i = 0; i < (k ? 4 : 2); ++i)
-    if (!rope_strides(given[i], B, i < 2 ? Hq : Hk, N, D, s[i])) return CALIBATT_ERR_SHAPE;
+    if (!rope_strides(given[i], B, i < 2 ? Hq : Hk, N, D, i & 1, s[i])) return CALIBATT_ERR_SHAPE;
   if (((uintptr_t)q | (uintptr_t)q_out | (uintptr_t)k | (uintptr_t)(k ? k_out : nullptr)) & 15) return CALIBATT_ERR_SHAPE;
   if ((uintptr_t)rope->table & 7) return CALIBATT_ERR_SHAPE;
   const RopeTensor tq = {q, q_out, s[0], s[1], Hq}, tk = {k, k_out, s[2], s[3], Hk};
   p.units = halves ? p.pairs / 8 + (D - 2 * p.pairs) / 8 : D / 8;
   p.tokens_per_wg = 256 / p.units;
+  if (N / p.tokens_per_wg >= 0xffffff) return CALIBATT_ERR_SHAPE;  // a launch has less than 2^32 threads along an axis
   // Heads of one workgroup: as many as leave every CU eight workgroups, at most 16 (the tables are then read for one
   // byte in sixteen that is moved).
   const long long wgs = (long long)B * ((N + p.tokens_per_wg - 1) / p.tokens_per_wg);
@@ -300,12 +304,12 @@ extern "C" int calibatt_layer_norm_fwd(const void *x, const void *weight, const 
   const calibatt_strides packed = {H * N * C, N * C, C};
   const calibatt_strides &sx = x_strides ? *x_strides : packed, &sy = y_strides ? *y_strides : packed;
   const int bytes = element_bytes(dtype), wbytes = element_bytes(weight_dtype);
-  if (!norm_tensor_ok(x, sx, bytes) || !norm_tensor_ok(y, sy, bytes)) return CALIBATT_ERR_SHAPE;
-  if (((uintptr_t)weight | (uintptr_t)bias) & (wbytes - 1)) return CALIBATT_ERR_SHAPE;
   const int64_t n[3] = {B, H, N};
+  if (!norm_tensor_ok(x, n, sx, bytes, 0) || !norm_tensor_ok(y, n, sy, bytes, C)) return CALIBATT_ERR_SHAPE;
+  if (((uintptr_t)weight | (uintptr_t)bias) & (wbytes - 1)) return CALIBATT_ERR_SHAPE;
   const calibatt_strides *const s[3] = {&sx, &sx, &sy};
   NormDims p;
-  if (int st = norm_dims(n, s, C, eps, center, weight_dtype == CALIBATT_F32, p)) return st;
+  norm_dims(n, s, C, eps, center, weight_dtype == CALIBATT_F32, p);
   const bool wide = norm_wide(x, sx, C, bytes) && norm_wide(y, sy, C, bytes) && (((uintptr_t)weight | (uintptr_t)bias) & 15) == 0;
   const NormTensors t = {x, nullptr, y};
   hipStream_t hs = (hipStream_t)stream;
@@ -335,7 +339,9 @@ extern "C" int calibatt_layer_norm_bwd(const void *dy, const void *x, const void
   const calibatt_strides &sg = dy_strides ? *dy_strides : packed, &sx = x_strides ? *x_strides : packed,
                          &sd = dx_strides ? *dx_strides : packed;
   const int bytes = element_bytes(dtype), wbytes = element_bytes(weight_dtype);
-  if (!norm_tensor_ok(dy, sg, bytes) || !norm_tensor_ok(x, sx, bytes) || !norm_tensor_ok(dx, sd, bytes)) return CALIBATT_ERR_SHAPE;
+  const int64_t n[3] = {B, H, N};
+  if (!norm_tensor_ok(dy, n, sg, bytes, 0) || !norm_tensor_ok(x, n, sx, bytes, 0) || !norm_tensor_ok(dx, n, sd, bytes, C))
+    return CALIBATT_ERR_SHAPE;
   if (((uintptr_t)weight | (uintptr_t)dweight | (uintptr_t)dbias) & (wbytes - 1)) return CALIBATT_ERR_SHAPE;
   const bool params = dweight || dbias;
   if (params) {
@@ -344,10 +350,9 @@ extern "C" int calibatt_layer_norm_bwd(const void *dy, const void *x, const void
     if ((uintptr_t)workspace & 3) return CALIBATT_ERR_SHAPE;
     if (workspace_bytes < need) return CALIBATT_ERR_BUFFER_TOO_SMALL;
   }
-  const int64_t n[3] = {B, H, N};
   const calibatt_strides *const s[3] = {&sx, &sg, &sd};
   NormDims p;
-  if (int st = norm_dims(n, s, C, eps, center, weight_dtype == CALIBATT_F32, p)) return st;
+  norm_dims(n, s, C, eps, center, weight_dtype == CALIBATT_F32, p);
   const bool wide = norm_wide(x, sx, C, bytes) && norm_wide(dy, sg, C, bytes) && norm_wide(dx, sd, C, bytes) &&
                     (((uintptr_t)weight | (uintptr_t)workspace) & 15) == 0;
   const NormTensors t = {x, dy, dx};

@@ -15,6 +15,7 @@ using namespace calibatt_host;
 
 constexpr int WINDOW_CUS = 256;        // plans are functions of the sizes alone
 constexpr int WINDOW_MAX_PARTS = 64;
+constexpr int64_t MAX_GRID = 0x7ffff0;  // workgroups: a launch has less than 2^32 threads, 512 to a workgroup at most
 
 // Keys that n neighbouring queries see at most, without the sinks.
 int64_t window_span(const calibatt_window &w, int n, int Nk) {
@@ -59,18 +60,20 @@ int window_check(int B, int Hq, int Hkv, int Nq, int Nk, int D, const calibatt_w
   return CALIBATT_OK;
 }
 
-// Strides of a tensor; those of an axis of one entry are never stepped along.
-bool window_strides(const calibatt_strides *given, int B, int H, int N, int D, Strides &s) {
+// Strides of a tensor; those of an axis of one entry are never stepped along.  No two rows of an output may start in one.
+bool window_strides(const calibatt_strides *given, int B, int H, int N, int D, bool output, Strides &s) {
   s = given ? Strides{given->b, given->h, given->n} : Strides{(int64_t)H * N * D, (int64_t)N * D, D};
+  if (output && ((B > 1 && s.b < D) || (H > 1 && s.h < D))) return false;
   if (B == 1) s.b = 0;
   if (H == 1) s.h = 0;
   if (N == 1) s.n = D;
   if (s.n < D || s.b < 0 || s.h < 0 || s.n % 8 || s.h % 8 || s.b % 8) return false;
-  // rows of one head are addressed with 32-bit byte offsets
-  return (unsigned long long)(N - 1) * (unsigned long long)s.n * 2 + (unsigned long long)D * 2 <= 0xffffffffULL;
+  // The kernels address the rows of one head with 32-bit byte offsets, also those behind the last one that a tile or a block
+  // of 256 still has: they have to lie behind a descriptor's end, and not past 2^32 at the head's first rows again.
+  return ((unsigned long long)N + 256) * (unsigned long long)s.n * 2 <= 0xffffffffULL;
 }
 
-int window_dims(int B, int Hq, int Hkv, int Nq, int Nk, const calibatt_window &w, float scale, WindowDims &p) {
+void window_dims(int B, int Hq, int Hkv, int Nq, int Nk, const calibatt_window &w, float scale, WindowDims &p) {
   p = WindowDims{};
   p.B = B;
   p.Hq = Hq;
@@ -88,7 +91,6 @@ int window_dims(int B, int Hq, int Hkv, int Nq, int Nk, const calibatt_window &w
   p.scale = scale;
   p.scale_log2e = scale * 1.4426950408889634f;
   p.parts = 1;
-  return CALIBATT_OK;
 }
 
 template <int D, typename T>
@@ -96,7 +98,7 @@ int launch_forward(const uint16_t *q, const uint16_t *k, const uint16_t *v, uint
                    hipStream_t stream) {
   const bool step = is_step(p.Hq, p.Hkv, p.Nq);
   const int64_t units = (int64_t)p.B * (step ? p.Hkv : p.Hq * ((p.Nq + 127) / 128)) * p.parts;
-  if (units > 0x7ffffff0LL) return CALIBATT_ERR_SHAPE;
+  if (units > MAX_GRID) return CALIBATT_ERR_SHAPE;
   const unsigned grid = (unsigned)(8 * ((units + 7) / 8));
   int unused = 0, st;
   if (step) {
@@ -181,7 +183,7 @@ int launch_backward(const GradTensors &t, const WindowDims &p, hipStream_t strea
   const int64_t cut = p.bwd_parts > 1 ? p.Nk : p.bwd_sink_parts > 1 ? std::min(p.Nk, p.n_sink_blocks * BLOCK) : 0;
   const int64_t sums = 2 * cut * p.B * p.Hkv + (p.dq_parts > 1 ? (int64_t)p.B * p.Hq * p.Nq : 0);
   const int64_t per_wg = 256 / (D / 8), sum_wgs = (sums + per_wg - 1) / per_wg;
-  if (q_units > 0x7ffffff0LL || k_units > 0x7ffffff0LL || sum_wgs > 0x7fffffffLL) return CALIBATT_ERR_SHAPE;
+  if (q_units > MAX_GRID || k_units > MAX_GRID || sum_wgs > MAX_GRID) return CALIBATT_ERR_SHAPE;
   if (int st = launch_kernel(window_attn_dq_kernel<D, T>, (unsigned)(8 * ((q_units + 7) / 8)), 256, DQ_LDS, stream, t.dout, t.q, t.k,
                              t.v, t.out, t.lse, t.dq, t.stats, p))
     return st;
@@ -213,8 +215,8 @@ extern "C" int calibatt_window_attn_fwd(const void *q, const void *k, const void
   if (out == q || out == k || out == v || !(scale - scale == 0.f)) return CALIBATT_ERR_SHAPE;
   WindowDims p;
   window_dims(B, Hq, Hkv, Nq, Nk, *window, scale, p);
-  if (!window_strides(q_strides, B, Hq, Nq, D, p.q) || !window_strides(kv_strides, B, Hkv, Nk, D, p.kv) ||
-      !window_strides(out_strides, B, Hq, Nq, D, p.out))
+  if (!window_strides(q_strides, B, Hq, Nq, D, false, p.q) || !window_strides(kv_strides, B, Hkv, Nk, D, false, p.kv) ||
+      !window_strides(out_strides, B, Hq, Nq, D, true, p.out))
     return CALIBATT_ERR_SHAPE;
   if ((((uintptr_t)q | (uintptr_t)k | (uintptr_t)v | (uintptr_t)out | (uintptr_t)workspace) & 15) || ((uintptr_t)lse & 3))
     return CALIBATT_ERR_SHAPE;
@@ -252,9 +254,9 @@ extern "C" int calibatt_window_attn_bwd(const void *dout, const void *q, const v
   if (dq == dk || dq == dv) return CALIBATT_ERR_SHAPE;
   WindowDims p;
   window_dims(B, Hq, Hkv, Nq, Nk, *window, scale, p);
-  if (!window_strides(dout_strides, B, Hq, Nq, D, p.dout) || !window_strides(q_strides, B, Hq, Nq, D, p.q) ||
-      !window_strides(kv_strides, B, Hkv, Nk, D, p.kv) || !window_strides(out_strides, B, Hq, Nq, D, p.out) ||
-      !window_strides(dq_strides, B, Hq, Nq, D, p.dq) || !window_strides(dkv_strides, B, Hkv, Nk, D, p.dkv))
+  if (!window_strides(dout_strides, B, Hq, Nq, D, false, p.dout) || !window_strides(q_strides, B, Hq, Nq, D, false, p.q) ||
+      !window_strides(kv_strides, B, Hkv, Nk, D, false, p.kv) || !window_strides(out_strides, B, Hq, Nq, D, false, p.out) ||
+      !window_strides(dq_strides, B, Hq, Nq, D, true, p.dq) || !window_strides(dkv_strides, B, Hkv, Nk, D, true, p.dkv))
     return CALIBATT_ERR_SHAPE;
   uintptr_t at = 0;
   for (const void *x : {dout, q, k, v, out, (const void *)dq, (const void *)dk, (const void *)dv, (const void *)workspace}) at |= (uintptr_t)x;

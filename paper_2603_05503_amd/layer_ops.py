@@ -337,14 +337,16 @@ class Window:
         for name, v in values.items():
             if not -(2 ** 31) <= int(v) < 2 ** 31:
                 raise ValueError(f"{name} does not fit 32 bits")
-        self.left, self.right, self.sinks, self.frame, self.offset = self._values = tuple(int(v) for v in values.values())
+        self._values = tuple(int(v) for v in values.values())  # (not to be changed: what is known of a call's sizes hangs on them)
         self._bytes = {}  # sizes of a call -> workspace bytes of its forward and of its gradients
+
+    left, right, sinks, frame, offset = (property(lambda self, i=i: self._values[i]) for i in range(5))
 
     def _c(self, q_start, q_len, k_len, B, device):
         """The C struct of one call."""
         import torch
 
-        c = _CWindow(self.left, self.right, self.sinks, self.frame, self.offset)
+        c = _CWindow(*self._values)
         for name, t in (("q_start", q_start), ("q_len", q_len), ("k_len", k_len)):
             if t is not None:
                 if not (t.device == device and t.dtype == torch.int32 and t.dim() == 1 and t.shape[0] == B and t.is_contiguous()):
@@ -357,7 +359,7 @@ class Window:
         key = (B, Hq, Hkv, Nq, Nk, D)
         n = self._bytes.get(key)
         if n is None:
-            c, fwd, bwd = _CWindow(self.left, self.right, self.sinks, self.frame, self.offset), C.c_int64(0), C.c_int64(0)
+            c, fwd, bwd = _CWindow(*self._values), C.c_int64(0), C.c_int64(0)
             st = _b.load_library().calibatt_window_attn_workspace_bytes(*key, C.addressof(c), C.byref(fwd), C.byref(bwd))
             if st != 0:
                 raise _b.CalibattError(st, "calibatt_window_attn_workspace_bytes")

@@ -52,13 +52,14 @@ def test_rope_table_refusals(n, dims, lengths, theta, status):
 
 
 def _rope(q=P, qo=P, k=P, ko=P, B=1, Hq=2, Hk=2, N=64, D=64, dims=(32, 16, 16), length=(4, 4, 4), grid=(4, 4, 4), start=(0, 0, 0),
-          interleaved=1, positions=None, positions_b=0, sq=None, dtype=0, table=P):
+          interleaved=1, positions=None, positions_b=0, sq=None, so=None, dtype=0, table=P):
     pad = lambda x: (C.c_int32 * 4)(*x)  # noqa: E731
     r = _CRope(len(dims), interleaved, pad(dims), pad(length), table)
     place = _CRopePlace(pad(grid), pad(start), positions, positions_b)
-    s = None if sq is None else (C.c_int64 * 3)(*sq)
+    s, o = (None if x is None else (C.c_int64 * 3)(*x) for x in (sq, so))
     return pkg.load_library().calibatt_rope_axes(q, qo, k, ko, B, Hq, Hk, N, D, C.addressof(r), C.addressof(place),
-                                                 None if s is None else C.addressof(s), None, None, None, dtype, 0, None)
+                                                 None if s is None else C.addressof(s), None if o is None else C.addressof(o),
+                                                 None, None, dtype, 0, None)
 
 
 @pytest.mark.parametrize("kw,status", [
@@ -69,23 +70,26 @@ def _rope(q=P, qo=P, k=P, ko=P, B=1, Hq=2, Hk=2, N=64, D=64, dims=(32, 16, 16), 
     (dict(grid=(5, 4, 4)), SHAPE), (dict(grid=(4, 4, 0)), SHAPE), (dict(start=(1, 0, 0)), SHAPE), (dict(start=(-1, 0, 0)), SHAPE),
     (dict(N=63), SHAPE), (dict(q=P + 8), SHAPE), (dict(ko=P + 2), SHAPE), (dict(table=P + 4), SHAPE),
     (dict(positions=P + 2), SHAPE), (dict(positions=P, positions_b=-3), SHAPE),
-    (dict(sq=(8192, 4096, 60)), SHAPE), (dict(sq=(8192, 4096, 56)), SHAPE), (dict(sq=(8192, -4096, 64)), SHAPE)])
+    (dict(sq=(8192, 4096, 60)), SHAPE), (dict(sq=(8192, 4096, 56)), SHAPE), (dict(sq=(8192, -4096, 64)), SHAPE),
+    (dict(so=(8192, 0, 64)), SHAPE), (dict(B=2, so=(56, 4096, 64)), SHAPE), (dict(N=(1 << 30) + 1), SHAPE), (dict(N=1 << 30, D=1024), SHAPE)])
 def test_rope_refusals(kw, status):
     assert _rope(**kw) == status
 
 
-def _norm(fn, n=(2, 3, 4), C_=64, x=P, y=P, dy=P, w=P, b=P, eps=1e-6, dtype=0, wtype=0, dw=P, db=P, ws=P, nbytes=1 << 40):
+def _norm(fn, n=(2, 3, 4), C_=64, sy=None, x=P, y=P, dy=P, w=P, b=P, eps=1e-6, dtype=0, wtype=0, dw=P, db=P, ws=P, nbytes=1 << 40):
     lib = pkg.load_library()
+    sy = None if sy is None else (C.c_int64 * 3)(*sy)
     if fn == "fwd":
-        return lib.calibatt_layer_norm_fwd(x, w, b, y, *n, C_, None, None, eps, 1, dtype, wtype, None)
-    return lib.calibatt_layer_norm_bwd(dy, x, w, y, dw, db, *n, C_, None, None, None, eps, 1, dtype, wtype, ws, nbytes, None)
+        return lib.calibatt_layer_norm_fwd(x, w, b, y, *n, C_, None, sy, eps, 1, dtype, wtype, None)
+    return lib.calibatt_layer_norm_bwd(dy, x, w, y, dw, db, *n, C_, None, None, sy, eps, 1, dtype, wtype, ws, nbytes, None)
 
 
 @pytest.mark.parametrize("fn", ["fwd", "bwd"])
 @pytest.mark.parametrize("kw,status", [
     (dict(x=None), NULL), (dict(y=None), NULL), (dict(n=(0, 3, 4)), SHAPE), (dict(n=(2, 3, -1)), SHAPE), (dict(C_=0), SHAPE),
     (dict(n=(1 << 20, 1 << 20, 1)), SHAPE), (dict(C_=8193), UNSUPPORTED), (dict(dtype=3), UNSUPPORTED), (dict(wtype=1), UNSUPPORTED),
-    (dict(eps=-1.0), SHAPE), (dict(eps=math.nan), SHAPE), (dict(x=P + 1), SHAPE), (dict(w=P + 1), SHAPE), (dict(wtype=2, w=P + 2), SHAPE)])
+    (dict(eps=-1.0), SHAPE), (dict(eps=math.nan), SHAPE), (dict(x=P + 1), SHAPE), (dict(w=P + 1), SHAPE), (dict(wtype=2, w=P + 2), SHAPE),
+    (dict(sy=(768, 256, 0)), SHAPE), (dict(sy=(768, 63, 256)), SHAPE), (dict(sy=(-1, 256, 64)), SHAPE)])
 def test_norm_refusals(fn, kw, status):
     assert _norm(fn, **kw) == status
 
@@ -157,9 +161,40 @@ def test_window_size_refusals(kw, status):
     (dict(q=None), NULL), (dict(k=None), NULL), (dict(v=None), NULL), (dict(out=None), NULL), (dict(out=P), SHAPE),
     (dict(scale=math.inf), SHAPE), (dict(scale=math.nan), SHAPE), (dict(dtype=2), UNSUPPORTED), (dict(q=P + 8), SHAPE),
     (dict(lse=P + 2), SHAPE), (dict(sq=(1 << 20, 1 << 14, 60)), SHAPE), (dict(skv=(1 << 20, 1 << 14, 68)), SHAPE),
-    (dict(so=(-8, 1 << 14, 64)), SHAPE), (dict(skv=(0, 0, 1 << 24)), SHAPE), (dict(ws=P, nbytes=0, Nk=4096, left=-1), TOO_SMALL)])
+    (dict(so=(-8, 1 << 14, 64)), SHAPE), (dict(so=(1 << 20, 0, 64)), SHAPE), (dict(so=(0, 1 << 14, 64)), SHAPE),
+    (dict(skv=(0, 0, 0xffffffff // 2 // 300 & ~7)), SHAPE), (dict(skv=(0, 0, 1 << 24)), SHAPE), (dict(ws=P, nbytes=0, Nk=4096, left=-1), TOO_SMALL)])
 def test_window_forward_refusals(kw, status):
     assert _window("fwd", **kw) == status
+
+
+def _window_bwd(B=2, Hq=4, Hkv=2, Nq=300, Nk=300, D=64, left=10, frame=1, dout=P, q=2 * P, k=3 * P, v=4 * P, out=5 * P, lse=6 * P,
+                dq=7 * P, dk=8 * P, dv=9 * P, scale=1.0, dtype=0, s=(), ws=10 * P, nbytes=1 << 40):
+    from paper_2603_05503_amd.layer_ops import _CWindow
+
+    w = _CWindow(left, 0, 0, frame, 0, None, None, None)
+    names = ("dout", "q", "kv", "out", "dq", "dkv")
+    arrays = {n: (C.c_int64 * 3)(*x) for n, x in dict(s).items()}
+    return pkg.load_library().calibatt_window_attn_bwd(
+        dout, q, k, v, out, lse, dq, dk, dv, B, Hq, Hkv, Nq, Nk, D, C.addressof(w), scale,
+        *(C.addressof(arrays[n]) if n in arrays else None for n in names), dtype, ws, nbytes, None)
+
+
+@pytest.mark.parametrize("kw,status", [({name: None}, NULL) for name in ("dout", "q", "k", "v", "out", "lse", "dq", "dk", "dv", "ws")] + [
+    (dict(Hq=3), SHAPE), (dict(Nk=0), SHAPE), (dict(D=96), UNSUPPORTED), (dict(dtype=2), UNSUPPORTED), (dict(frame=0), SHAPE),
+    (dict(scale=math.inf), SHAPE), (dict(dk=9 * P), SHAPE), (dict(dq=8 * P), SHAPE), (dict(dq=2 * P), SHAPE), (dict(dv=4 * P), SHAPE),
+    (dict(dk=P), SHAPE), (dict(ws=5 * P), SHAPE), (dict(lse=6 * P + 2), SHAPE), (dict(dv=9 * P + 8), SHAPE), (dict(ws=10 * P + 4), SHAPE),
+    (dict(s=(("q", (1 << 20, 1 << 14, 60)),)), SHAPE), (dict(s=(("dout", (1 << 20, 1 << 14, 68)),)), SHAPE),
+    (dict(s=(("dq", (1 << 20, 0, 64)),)), SHAPE), (dict(s=(("dkv", (0, 1 << 15, 64)),)), SHAPE),
+    (dict(s=(("kv", (0, 0, 0xffffffff // 2 // 300 & ~7)),)), SHAPE), (dict(nbytes=2 * 4 * 300 * 8 - 1), TOO_SMALL)])
+def test_window_gradient_refusals(kw, status):
+    assert _window_bwd(**kw) == status
+
+
+def test_a_window_does_not_change():
+    w = pkg.Window(3, 1, 2, 5, -7)
+    assert (w.left, w.right, w.sinks, w.frame, w.offset) == (3, 1, 2, 5, -7)
+    with pytest.raises(AttributeError):
+        w.left = 4
 
 
 def test_window_workspace_follows_the_work():
