@@ -24,6 +24,10 @@
  * forward reads directly), calibatt_merge_intervals(),
  * calibatt_share_timesteps().
  *
+ * Around the attention of a layer: calibatt_rope_axes() (rotary positions with
+ * several axes), calibatt_layer_norm_fwd() / _bwd(), calibatt_window_attn_fwd() /
+ * _bwd() (attention in a window with first keys that stay visible).
+ *
  * Plain C, no exceptions cross the boundary, every buffer is owned by the
  * caller, and the library allocates no device memory (scratch comes in through
  * workspace arguments).  Nothing in the environment changes what a call does.

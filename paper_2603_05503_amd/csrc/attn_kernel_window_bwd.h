@@ -16,7 +16,8 @@
 // barrier; the second wave of the SIMD fills what one leaves.  Us of dQ, and of dK and dV, for 16 380 tokens, 8 query heads
 // on 4 key heads, D = 128, nine frames of 780 and the first: scheduled by the compiler, 64 columns to a wave, one wave per
 // SIMD 930 and 2660 (it gathers reads and vector work and spills), the same in gaps 787 and 1253 (half its cycles waits),
-// this form 655 and 990.
+// this form 642 and 940.  Of a gap's about 125 cycles (dQ) and 142 (dK, dV) on a CU, its eight waves' MFMAs take 64 of each
+// SIMD, and their operands, 1 KB a wave and 1.25 KB with K's, 64 and 80 of LDS: 32 columns to a wave feed no more.
 #pragma once
 #include "attn_kernel_window.h"
 
