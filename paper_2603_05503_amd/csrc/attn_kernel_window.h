@@ -272,8 +272,8 @@ __global__ __launch_bounds__(256, 2) __attribute__((amdgpu_num_vgpr(IL_VGPRS))) 
 }
 
 // ---- few queries --------------------------------------------------------------------------------------------
-// Up to 32 rows of queries share their keys: the G query heads of a key head with Nq queries each, a single token of
-// a stream above all.  What such a call costs is reading the visible keys and values once.  A workgroup takes a part of
+// Up to 32 rows of queries share their keys: SHARED, the G query heads of a key head with Nq queries each, a single token of
+// a stream above all; or a block of 32 queries of one head, where blocks of 128 would leave the GPU idle (forward_form).  What such a call costs is reading the visible keys and values once.  A workgroup takes a part of
 // a (batch entry, key head)'s tiles of 32 keys, each of its four waves every fourth of them, in LDS of its own, so that
 // the loop has no barrier: S^T = K Q^T and O^T += V^T P^T as in the engine for blocks, with all rows in one 32-column
 // MFMA tile.  Two tiles of K and V per wave are in flight (64 KB a CU at D = 128), which is what HBM's latency asks for.
@@ -288,7 +288,7 @@ struct StepLds {
   static_assert(STEP_WAVES * 32 * (JOIN_STRIDE + 2) * 4 <= BYTES, "the joined sums do not fit");
 };
 
-template <int D, typename T>
+template <int D, bool SHARED, typename T>
 __global__ __launch_bounds__(STEP_WAVES * 64) void window_attn_step_kernel(
     const uint16_t *__restrict__ gq, const uint16_t *__restrict__ gk, const uint16_t *__restrict__ gv,
     uint16_t *__restrict__ gout, float *__restrict__ lse, const WindowDims p) {
@@ -298,25 +298,29 @@ __global__ __launch_bounds__(STEP_WAVES * 64) void window_attn_step_kernel(
   using LoadV = TileLoader<D, STEP_KEYS, 64, true>;
   constexpr int ROWB = D * 2, DS = D / 16, DB = D / 32, ITERS = LoadK::ITERS;
   extern __shared__ __attribute__((aligned(1024))) char lds[];
-  const int unit = window_unit(p.B * p.Hkv * p.parts);
+  const int G = p.Hq / p.Hkv, blocks = SHARED ? 1 : (p.Nq + 31) / 32;
+  const int unit = window_unit(p.B * (SHARED ? p.Hkv : p.Hq) * blocks * p.parts);
   if (unit < 0) return;
-  const int part = unit % p.parts;
-  int b, hk;
-  window_head(unit / p.parts, p.B, 1, b, hk);
-  const int G = p.Hq / p.Hkv, R = G * p.Nq;
+  const int part = unit % p.parts, x = unit / p.parts / blocks, block = blocks - 1 - (unit / p.parts - x * blocks);
+  int b, h0;  // the first head of the rows
+  window_head(x, p.B, SHARED ? 1 : G, b, h0);
+  const int hk = SHARED ? h0 : h0 / G, i0 = 32 * block, R = SHARED ? G * p.Nq : min(32, p.Nq - i0);
+  if (SHARED) h0 *= G;
+  auto head_of = [&](int row) { return SHARED ? h0 + row / p.Nq : h0; };
+  auto query_of = [&](int row) { return SHARED ? row % p.Nq : i0 + row; };
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l32 = lane & 31, g = lane >> 5;
   const WindowEntry e(p, b);
-  const int row = min(l32, R - 1), h = hk * G + row / p.Nq, i = row % p.Nq;
+  const int row = min(l32, R - 1), h = head_of(row);
   f32x16 o[DB];
 #pragma unroll
   for (int db = 0; db < DB; ++db)
 #pragma unroll
     for (int v = 0; v < 16; ++v) o[db][v] = 0.f;
   float m_run = -FLT_MAX, l_run = 0.f;
-  if (e.q_len > 0) {
-    const Tiles tiles(p, e, 0, e.q_len);
+  if (i0 < e.q_len) {
+    const Tiles tiles(p, e, i0, SHARED ? e.q_len : min(i0 + 32, e.q_len));
     int lo, hi;
-    const int row_q = min(i, e.q_len - 1);
+    const int row_q = min(query_of(row), e.q_len - 1);
     e.interval(p, row_q, lo, hi);
     const int t0 = (int)((long long)tiles.n * part / p.parts), t1 = (int)((long long)tiles.n * (part + 1) / p.parts);
     const size_t kv_head = (size_t)b * p.kv.b + (size_t)hk * p.kv.h;
@@ -424,7 +428,7 @@ __global__ __launch_bounds__(STEP_WAVES * 64) void window_attn_step_kernel(
   constexpr int LANES = D / 8;  // 8 channels each
   for (int L = threadIdx.x; L < R * LANES; L += STEP_WAVES * 64) {
     const int rr = L / LANES, c = 8 * (L % LANES);
-    const int head = hk * G + rr / p.Nq, qi = rr % p.Nq;
+    const int head = head_of(rr), qi = query_of(rr);
     float m = -FLT_MAX, l = 0.f, x[8];
 #pragma unroll
     for (int w = 0; w < STEP_WAVES; ++w) m = fmaxf(m, ml[2 * (w * 32 + rr)]);

@@ -28,20 +28,38 @@ int64_t window_tiles(const calibatt_window &w, int n, int Nk, int tile) {
   return (std::min<int64_t>(w.sinks, Nk) + tile - 1) / tile + (window_span(w, n, Nk) + tile - 1) / tile;
 }
 
-// Few enough rows of queries to a key head to go through the kernel that reads keys once for all of them.
-bool is_step(int Hq, int Hkv, int Nq) { return (int64_t)(Hq / Hkv) * Nq <= 32; }
+// Which kernel a forward goes through.
+enum ForwardForm { BLOCKS_128, BLOCKS_32, SHARED_ROWS };
+// Workgroups of the kernel for few queries that the GPU holds (its LDS, 128 KB at D = 128).
+int64_t step_slots(int D) { return D == 128 ? WINDOW_CUS : 2 * WINDOW_CUS; }
+ForwardForm forward_form(int B, int Hq, int Hkv, int Nq, int Nk, int D, const calibatt_window &w) {
+  // few enough rows of queries to a key head to read the keys once for all of them
+  if ((int64_t)(Hq / Hkv) * Nq <= 32) return SHARED_ROWS;
+  // Calls whose blocks of 128 queries leave most of the GPU idle wait for one chain of tiles after the other; blocks of 32,
+  // whose four waves take a fourth of the keys each, have four times as many chains of half the length, but read every key
+  // four times as often.  They are faster where they all run at once, for up to about 48 tiles each.  Us, D = 64 / 128, all
+  // keys so far, blocks of 128 (in parts) and of 32: 2 heads of 128 queries on 1024 keys 16 and 12 / 18 and 16; 8 heads of
+  // 1024 17 and 12 / 22 and 17; 8 of 1024 on 4096 27.5 and 27.8 / 33 and 54; 16 of 1024 19 and 15 / 26 and 22 (two rounds:
+  // not taken), on 3000 30 and 34 / 40 and 64.
+  const int64_t units = (int64_t)B * Hq * ((Nq + 31) / 32);
+  if (units <= step_slots(D) && units * window_tiles(w, 32, Nk, STEP_KEYS) <= 48 * step_slots(D)) return BLOCKS_32;
+  return BLOCKS_128;
+}
 
 // Pieces that the tiles of every block of queries are cut into.
-int forward_parts(int B, int Hq, int Hkv, int Nq, int Nk, const calibatt_window &w) {
-  if (is_step(Hq, Hkv, Nq)) {
-    const int64_t units = (int64_t)B * Hkv, tiles = window_tiles(w, Nq, Nk, STEP_KEYS);
+int forward_parts(ForwardForm form, int B, int Hq, int Hkv, int Nq, int Nk, int D, const calibatt_window &w) {
+  if (form != BLOCKS_128) {
+    const bool shared = form == SHARED_ROWS;
+    const int64_t units = shared ? (int64_t)B * Hkv : (int64_t)B * Hq * ((Nq + 31) / 32);
+    const int64_t tiles = window_tiles(w, shared ? Nq : 32, Nk, STEP_KEYS);
     if (tiles <= 8 * STEP_WAVES) return 1;  // a second launch costs more than eight rounds of the waves
-    const int64_t fill = std::max<int64_t>(1, 2 * WINDOW_CUS / units);
+    // (few rows of one key head wait for HBM, and have two workgroups per CU one after the other)
+    const int64_t fill = std::max<int64_t>(1, (shared ? 2 * WINDOW_CUS : step_slots(D)) / units);
     return (int)std::max<int64_t>(1, std::min<int64_t>({fill, (tiles + 2 * STEP_WAVES - 1) / (2 * STEP_WAVES), WINDOW_MAX_PARTS}));
   }
   const int64_t units = (int64_t)B * Hq * ((Nq + 127) / 128), tiles = window_tiles(w, 128, Nk, 64);
-  // As many as fill the GPU, of eight tiles at least: 4 heads of 3000 tokens, all keys, 56 us whole, 40 in four parts; 8 heads
-  // of 875, three frames of 134, D = 64, 19 whole, 22 in two.
+  // As many as fill the GPU, of eight tiles at least: 4 heads of 3000 tokens, all keys, 54 us whole, 37 in five parts; 16 heads
+  // of 1024, D = 64, on 8192 keys 114 and, in four, 51, on 1024 keys 19.1 whole, 19.4 in two.
   const int64_t fill = 2 * WINDOW_CUS / units;
   return (int)std::max<int64_t>(1, std::min<int64_t>({fill, tiles / 8, WINDOW_MAX_PARTS}));
 }
@@ -94,24 +112,22 @@ void window_dims(int B, int Hq, int Hkv, int Nq, int Nk, const calibatt_window &
 }
 
 template <int D, typename T>
-int launch_forward(const uint16_t *q, const uint16_t *k, const uint16_t *v, uint16_t *out, float *lse, const WindowDims &p,
-                   hipStream_t stream) {
-  const bool step = is_step(p.Hq, p.Hkv, p.Nq);
-  const int64_t units = (int64_t)p.B * (step ? p.Hkv : p.Hq * ((p.Nq + 127) / 128)) * p.parts;
+int launch_forward(ForwardForm form, const uint16_t *q, const uint16_t *k, const uint16_t *v, uint16_t *out, float *lse,
+                   const WindowDims &p, hipStream_t stream) {
+  const int block = form == BLOCKS_128 ? 128 : 32;
+  const int64_t units = (int64_t)p.B * (form == SHARED_ROWS ? p.Hkv : (int64_t)p.Hq * ((p.Nq + block - 1) / block)) * p.parts;
   if (units > MAX_GRID) return CALIBATT_ERR_SHAPE;
   const unsigned grid = (unsigned)(8 * ((units + 7) / 8));
-  int unused = 0, st;
-  if (step) {
-    static DevInfo info;
-    constexpr int SMEM = StepLds<D, T>::BYTES;
-    if ((st = prepare(window_attn_step_kernel<D, T>, STEP_WAVES * 64, SMEM, info, unused))) return st;
-    st = launch_kernel(window_attn_step_kernel<D, T>, grid, STEP_WAVES * 64, SMEM, stream, q, k, v, out, lse, p);
-  } else {
-    static DevInfo info;
-    constexpr int SMEM = WindowRow<D, T>::LDS_BYTES;
-    if ((st = prepare(window_attn_fwd_kernel<D, T>, 256, SMEM, info, unused))) return st;
-    st = launch_kernel(window_attn_fwd_kernel<D, T>, grid, 256, SMEM, stream, q, k, v, out, lse, p);
-  }
+  static DevInfo info[3];
+  auto go = [&](auto kernel, int threads, int smem) {
+    int unused = 0;
+    const int st = prepare(kernel, threads, smem, info[form], unused);
+    return st ? st : launch_kernel(kernel, grid, threads, smem, stream, q, k, v, out, lse, p);
+  };
+  constexpr int STEP_LDS = StepLds<D, T>::BYTES;
+  const int st = form == SHARED_ROWS ? go(window_attn_step_kernel<D, true, T>, STEP_WAVES * 64, STEP_LDS)
+                 : form == BLOCKS_32 ? go(window_attn_step_kernel<D, false, T>, STEP_WAVES * 64, STEP_LDS)
+                                     : go(window_attn_fwd_kernel<D, T>, 256, WindowRow<D, T>::LDS_BYTES);
   if (st || p.parts == 1) return st;
   const int64_t rows = (int64_t)p.B * p.Hq * p.Nq;
   constexpr int PER_WG = 256 / (D / 8);
@@ -199,7 +215,8 @@ extern "C" int calibatt_window_attn_workspace_bytes(int B, int Hq, int Hkv, int 
                                                     const calibatt_window *window, int64_t *forward, int64_t *backward) {
   if (!window || !forward || !backward) return CALIBATT_ERR_NULL;
   if (int st = window_check(B, Hq, Hkv, Nq, Nk, D, *window)) return st;
-  *forward = forward_bytes(forward_parts(B, Hq, Hkv, Nq, Nk, *window), B, Hq, Nq, D);
+  const ForwardForm form = forward_form(B, Hq, Hkv, Nq, Nk, D, *window);
+  *forward = forward_bytes(forward_parts(form, B, Hq, Hkv, Nq, Nk, D, *window), B, Hq, Nq, D);
   *backward = grad_plan(B, Hq, Hkv, Nq, Nk, D, *window).bytes;
   return CALIBATT_OK;
 }
@@ -220,8 +237,9 @@ extern "C" int calibatt_window_attn_fwd(const void *q, const void *k, const void
     return CALIBATT_ERR_SHAPE;
   if ((((uintptr_t)q | (uintptr_t)k | (uintptr_t)v | (uintptr_t)out | (uintptr_t)workspace) & 15) || ((uintptr_t)lse & 3))
     return CALIBATT_ERR_SHAPE;
+  const ForwardForm form = forward_form(B, Hq, Hkv, Nq, Nk, D, *window);
   if (workspace) {
-    p.parts = forward_parts(B, Hq, Hkv, Nq, Nk, *window);
+    p.parts = forward_parts(form, B, Hq, Hkv, Nq, Nk, D, *window);
     if (workspace_bytes < forward_bytes(p.parts, B, Hq, Nq, D)) return CALIBATT_ERR_BUFFER_TOO_SMALL;
     p.part_rows = (float *)workspace;
     p.part_ml = p.part_rows + (size_t)p.parts * B * Hq * Nq * D;
@@ -230,10 +248,10 @@ extern "C" int calibatt_window_attn_fwd(const void *q, const void *k, const void
   uint16_t *const o_ = (uint16_t *)out;
   hipStream_t s = (hipStream_t)stream;
   if (D == 128)
-    return dtype == CALIBATT_BF16 ? launch_forward<128, Bf16>(q_, k_, v_, o_, lse, p, s)
-                                  : launch_forward<128, F16>(q_, k_, v_, o_, lse, p, s);
-  return dtype == CALIBATT_BF16 ? launch_forward<64, Bf16>(q_, k_, v_, o_, lse, p, s)
-                                : launch_forward<64, F16>(q_, k_, v_, o_, lse, p, s);
+    return dtype == CALIBATT_BF16 ? launch_forward<128, Bf16>(form, q_, k_, v_, o_, lse, p, s)
+                                  : launch_forward<128, F16>(form, q_, k_, v_, o_, lse, p, s);
+  return dtype == CALIBATT_BF16 ? launch_forward<64, Bf16>(form, q_, k_, v_, o_, lse, p, s)
+                                : launch_forward<64, F16>(form, q_, k_, v_, o_, lse, p, s);
 }
 
 extern "C" int calibatt_window_attn_bwd(const void *dout, const void *q, const void *k, const void *v, const void *out,

@@ -151,6 +151,42 @@ def test_window_forward_with_lengths(lib, B, Hq, Hkv, Nq, Nk, D, c, start, q_len
     check_forward(out, lse, q, k, v, see, scale, dtype)
 
 
+# few blocks over many keys: cut along the keys
+@pytest.mark.parametrize("B,Hq,Hkv,Nq,Nk,D,c,start,q_len,k_len", [
+    (1, 2, 2, 100, 1700, 128, dict(left=-1, right=-1, sinks=0, frame=1), [0], [100], [1700]),
+    (2, 2, 1, 33, 4099, 64, dict(left=3000, right=0, sinks=50, frame=1), [4066, 1500], [33, 32], [4099, 1532]),
+    (1, 2, 2, 300, 2600, 128, dict(left=20, right=0, sinks=20, frame=100), [2300], [259], [2559]),
+    (3, 1, 1, 64, 3500, 64, dict(left=-1, right=0, sinks=0, frame=1), [3436, 0, -7], [64, 0, 64], [3500, 3500, 1])])
+@pytest.mark.parametrize("dtype", ["bfloat16", "float16"])
+def test_window_forward_of_few_blocks_over_many_keys(lib, B, Hq, Hkv, Nq, Nk, D, c, start, q_len, k_len, dtype):
+    assert lib.Window(**c).workspace_bytes(B, Hq, Hkv, Nq, Nk, D)[0] > 0
+    test_window_forward_with_lengths(lib, B, Hq, Hkv, Nq, Nk, D, c, start, q_len, k_len, dtype)
+
+
+@pytest.mark.parametrize("case", [i for i, x in enumerate(CASES) if x[3] > 32] + [-1 - i for i, x in enumerate(LENGTHS) if x[3] > 32])
+@pytest.mark.parametrize("dtype", ["bfloat16", "float16"])
+def test_window_forward_of_many_blocks(lib, case, dtype):
+    """The same calls among so many copies of themselves that they fill the GPU: the oracle's values for the first, its bits
+    for all others."""
+    torch = _torch()
+    B, Hq, Hkv, Nq, Nk, D, c = (CASES[case] if case >= 0 else LENGTHS[-1 - case])[:7]
+    start, q_len, k_len = (None,) * 3 if case >= 0 else LENGTHS[-1 - case][7:]
+    times = -(-600 // (B * Hq * -(-Nq // 32)))
+    print(f"many blocks {times} x {B} {Hq} {Hkv} {Nq} {Nk} {D} {c} {start} {q_len} {k_len} {dtype}", flush=True)
+    rng = np.random.default_rng(Nq + Nk + D)
+    q, k, v = make(rng, (B, Hq, Nq, D), dtype, 1.5), make(rng, (B, Hkv, Nk, D), dtype, 1.5), make(rng, (B, Hkv, Nk, D), dtype)
+    many = lambda t: t.repeat(times, *(1,) * (t.dim() - 1))  # noqa: E731
+    lengths = {}
+    if start is not None:
+        for name, x in (("q_start", start), ("q_len", q_len), ("k_len", k_len)):
+            lengths[name] = many(torch.tensor(np.array(x, dtype=np.int64).astype(np.int32), device="cuda"))
+        start = np.clip(start, -(2 ** 30), 2 ** 30)
+    out, lse = torch.full_like(many(q), 7.0), torch.full((B * times, Hq, Nq), 7.0, device="cuda")
+    lib.window_attn_fwd(many(q), many(k), many(v), out, lib.Window(**c), 0.11, lse=lse, **lengths)
+    check_forward(out[:B], lse[:B], q, k, v, visible(c, B, Nq, Nk, start, q_len, k_len), 0.11, dtype)
+    assert torch.equal(out, many(out[:B])) and torch.equal(lse, many(lse[:B]))
+
+
 @pytest.mark.parametrize("Nq", [1, 200])
 @pytest.mark.parametrize("gain", [1.0, 30.0])
 def test_window_large_logits_and_any_scale(lib, Nq, gain):
