@@ -850,7 +850,7 @@ int calibatt_window_attn_fwd(const void *q, const void *k, const void *v, void *
  * calibatt_window_attn_bwd: its gradients, for dout [B][Hq][Nq][D], the gradient
  * of out: dq like q, dk and dv [B][Hkv][Nk][D] (summed over the query heads that
  * share a key head; zeros for queries and keys that are not there or meet
- * nothing).  out and lse are the forward's for the same arguments.  S and dP are
+ * nothing, whose rows of q, dout, k and v may hold anything).  out and lse are the forward's for the same arguments.  S and dP are
  * formed twice, so that nothing is added up by atomics: the same inputs give the
  * same bits.  Sums are fp32; the probabilities and dS are rounded to the element
  * type for the products (fp16: times 2^15 and 2^4, dS may be up to 2^12).

@@ -234,8 +234,11 @@ __global__ __launch_bounds__(256, 2) void window_attn_dq_kernel(
     w.operand(gq + (size_t)b * p.q.b + (size_t)h * p.q.h + (size_t)row * p.q.n, q);
     w.operand(gdo + (size_t)b * p.dout.b + (size_t)h * p.dout.h + (size_t)row * p.dout.n, dout);
     const float z = lse[row0 + row];
-    // a query that sees nothing: exponents of -inf
-    const float lse2 = z == -INFINITY ? INFINITY : z * 1.4426950408889634f - GradScale<T>::P_LOG2;
+    // a query that sees nothing: exponents of -inf, and no dO, as a probability of zero does not outweigh what is not finite
+    const bool sees = z != -INFINITY;
+    const float lse2 = sees ? z * 1.4426950408889634f - GradScale<T>::P_LOG2 : INFINITY;
+#pragma unroll
+    for (int s = 0; s < DS; ++s) dout[s] = sees ? dout[s] : u32x4{0, 0, 0, 0};
     float dl = 0.f;
     {
       u32x4 o[DS];
@@ -492,6 +495,9 @@ __global__ __launch_bounds__(512, 2) void window_attn_dkv_kernel(
       const int jw0 = __builtin_amdgcn_readfirstlane(j0 + w.wave * Tile::COLS), jw1 = jw0 + Tile::COLS;
       const int from_max = jw1 <= j1 ? WindowQueries::first_of(p, e, jw1 - 1) : INT_MAX;
       const int to_min = jw1 <= p.sinks ? e.q_len : WindowQueries::end_of(p, e, max(jw0, p.sinks));
+      // no V for a key that nothing sees: it may hold anything, and dS = P (dP - delta) is zero only for a finite dP
+#pragma unroll
+      for (int s = 0; s < DS; ++s) v[s] = from < to ? v[s] : u32x4{0, 0, 0, 0};
       Tile::arrive(v);
       const float sc = p.scale_log2e == 0.f ? 1e-30f : p.scale_log2e, unseen = sc < 0.f ? INFINITY : -INFINITY;
       for (int u = u0; u < u1; ++u) {
