@@ -853,7 +853,8 @@ int calibatt_window_attn_fwd(const void *q, const void *k, const void *v, void *
  * nothing, whose rows of q, dout, k and v may hold anything).  out and lse are the forward's for the same arguments.  S and dP are
  * formed twice, so that nothing is added up by atomics: the same inputs give the
  * same bits.  Sums are fp32; the probabilities and dS are rounded to the element
- * type for the products (fp16: times 2^15 and 2^4, dS may be up to 2^12).
+ * type for the products (fp16: times 2^15, and times powers of two that the
+ * largest |dO| and |V| that meet anything allow, so that no dS overflows).
  * workspace: DEVICE, 16-byte aligned, calibatt_window_attn_workspace_bytes
  * (`backward`), needed always.  No result may be an input.
  * Errors: as calibatt_window_attn_fwd.

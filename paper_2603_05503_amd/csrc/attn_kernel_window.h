@@ -25,6 +25,8 @@ struct WindowDims {
   float *part_rows, *part_ml;              // [parts][B Hq Nq][D] sums and [parts][B Hq Nq][2] references and row sums
   int dq_parts, bwd_parts, bwd_sink_parts, n_sink_blocks;  // of the gradients, see attn_kernel_window_bwd.h
   float *part_dq, *part_dkv;
+  float *sizes;                            // [B Hkv][do_slots + v_slots], fp16: see GradScale
+  int do_slots, v_slots;
   Strides dout, dq, dkv;
 };
 

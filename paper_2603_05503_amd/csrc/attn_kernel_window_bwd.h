@@ -32,10 +32,19 @@ __device__ __forceinline__ int both_swz(int row) {
   return CH == 16 ? ((u & 3) << 2) | ((u >> 2) & 3) : ((u & 1) << 2) | ((u >> 1) & 3);
 }
 
-// fp16 has few exponents: probabilities are kept times 2^15, which takes 1 to 32768, and dS times 2^4 (up to 2^12 with its
-// precision down to 2^-18); bf16 needs neither.
-template <typename T> struct GradScale { static constexpr float P_LOG2 = 0.f, DS = 1.f; };
-template <> struct GradScale<F16> { static constexpr float P_LOG2 = 15.f, DS = 16.f; };
+// fp16 has few exponents: probabilities are kept times 2^15, which takes 1 to 32768, and dS times a power of two F that follows
+// the data (bf16 needs neither).  As out is a mean of rows of V, |dS| <= P (|dP| + |delta|) <= 2 |dO| |V|, and F is the largest
+// power of two that keeps twice that bound within 2^16: no dS leaves the type, whatever the scale of dO (a loss that was
+// scaled, say), and of a bound of one, dS down to 2^-28 keep their precision.  dQ's columns are queries, so F is a query's own
+// there; dK's are keys, whose sums need one F for all queries, that of the largest |dO| of the key head.
+template <typename T> struct GradScale { static constexpr float P_LOG2 = 0.f, P_UNIT = 1.f; static constexpr bool FOLLOWS = false; };
+template <> struct GradScale<F16> { static constexpr float P_LOG2 = 15.f, P_UNIT = 1.f / 32768.f; static constexpr bool FOLLOWS = true; };
+
+// F for squares of |dO| and of |V|
+__device__ __forceinline__ float grad_factor(float do_square, float v_square) {
+  const float bound = 2.f * sqrtf(do_square * v_square);  // (squares of up to 128 * 65504^2, products within fp32)
+  return bound > 0.f ? ldexpf(1.f, 15 - __builtin_amdgcn_frexp_expf(bound)) : 1.f;
+}
 
 // out (+)= a b.  Written out, because the compiler, given 512 registers, keeps every accumulator of an MFMA in AGPRs, from
 // where S and dP are copied element by element, and then moves the sums around them (700 copies per 128 MFMAs).  Here S
@@ -74,8 +83,6 @@ struct GradTile {
   // fills a tile, one for the matrix of its half.
   static constexpr int ITERS = ROWS * CH / NT, LOADS = ITERS ? 2 * ITERS : 1, RPI = NT / CH;
   static_assert((ITERS && RPI % 16 == 0) || 2 * ROWS * CH == NT, "the swizzle of an instruction's rows is the same for every one");
-  static constexpr float P_UNIT = GradScale<T>::P_LOG2 == 0.f ? 1.f : 1.f / 32768.f;  // what P_LOG2 stands for
-  static constexpr float DS_OF_P = GradScale<T>::DS * P_UNIT;                         // factor of dP - delta beside P as kept
 
   // A phase (S, dP, or one of the products that add up) has PH gaps.  The UNITS of vector work of 32 rows, pairs of a lane's
   // values, by their gap behind the start of dP: exponentials over 22/16 of a phase, then each pair's dS, in dK and dV's
@@ -178,6 +185,100 @@ struct GradTile {
   }
 };
 
+// dP - delta in units of dS beside P as kept
+__device__ __forceinline__ float ds_factor(float dp, float ds_of_p, float dl) { return __builtin_fmaf(dp, ds_of_p, -dl); }
+
+// The queries that see keys [j0, j1) (j1 within k_len): of the window between two positions, of the sinks all from the
+// first on.
+struct WindowQueries {
+  int begin, end;
+  // first query that sees key j, last + 1 that does
+  static __device__ __forceinline__ int first_of(const WindowDims &p, const WindowEntry &e, int j) {
+    if (p.right < 0) return 0;
+    const long long pos = ((long long)j / p.frame - p.right) * p.frame - e.start;
+    return (int)min(max(pos, 0ll), (long long)e.q_len);
+  }
+  static __device__ __forceinline__ int end_of(const WindowDims &p, const WindowEntry &e, int j) {
+    if (p.left < 0 || j < p.sinks) return e.q_len;
+    const long long pos = ((long long)j / p.frame + p.left + 1) * p.frame - e.start;
+    return (int)min(max(pos, 0ll), (long long)e.q_len);
+  }
+  __device__ __forceinline__ WindowQueries(const WindowDims &p, const WindowEntry &e, int j0, int j1) {
+    begin = first_of(p, e, j0);
+    end = j0 < p.sinks ? e.q_len : end_of(p, e, j1 - 1);
+  }
+};
+
+// ---- sizes of dO and V --------------------------------------------------------------------------------------
+// Largest squares of the norms of a key head's rows of dO (of the query heads that share it) and of V, of each in as many
+// pieces as there are slots.  Rows that meet nothing do not count, they may hold anything, nor do rows that are not finite:
+// those spoil what they meet, and nothing else.  Maxima: the order does not matter.  Reads dO and V once, beside kernels that
+// read them once for every block of queries or keys that meets them.
+constexpr int SIZE_ROWS = 128, SIZE_MAX_SLOTS = 128;  // rows of a piece at least, pieces of either tensor at most
+
+template <int D>
+__global__ __launch_bounds__(256) void window_attn_sizes_kernel(const uint16_t *__restrict__ gdo, const uint16_t *__restrict__ gv, const WindowDims p) {
+  constexpr int LANES = D / 8, ROWS = 256 / LANES;
+  __shared__ float most[4];
+  const int slots = p.do_slots + p.v_slots, bh = blockIdx.x / slots, slot = blockIdx.x - bh * slots, b = bh / p.Hkv, hk = bh - b * p.Hkv;
+  const int G = p.Hq / p.Hkv, c = 8 * (threadIdx.x % LANES);
+  const bool of_do = slot < p.do_slots;
+  const long long rows = of_do ? (long long)G * p.Nq : p.Nk;
+  const int piece = of_do ? slot : slot - p.do_slots, pieces = of_do ? p.do_slots : p.v_slots;
+  const long long first = rows * piece / pieces, last = rows * (piece + 1) / pieces;
+  const WindowEntry e(p, b);
+  float m = 0.f;
+#pragma unroll 2
+  for (long long r = first + threadIdx.x / LANES; r < last; r += ROWS) {
+    const uint16_t *row;
+    bool seen;
+    if (of_do) {
+      const int g = (int)(r / p.Nq), i = (int)(r - (long long)g * p.Nq);
+      int lo, hi;
+      e.interval(p, i, lo, hi);
+      seen = i < e.q_len && (lo < hi || min(p.sinks, hi) > 0);
+      row = gdo + (size_t)b * p.dout.b + (size_t)(hk * G + g) * p.dout.h + (size_t)i * p.dout.n;
+    } else {
+      const int j = (int)r;
+      seen = j < e.k_len && WindowQueries::first_of(p, e, j) < WindowQueries::end_of(p, e, j);
+      row = gv + (size_t)b * p.kv.b + (size_t)hk * p.kv.h + (size_t)j * p.kv.n;
+    }
+    const u32x4 raw = seen ? *reinterpret_cast<const u32x4 *>(row + c) : u32x4{0, 0, 0, 0};
+    float s = 0.f;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const uint32_t two = raw[k];
+      float x[2];
+      F16::unpack(two, x);
+      s = __builtin_fmaf(x[0], x[0], __builtin_fmaf(x[1], x[1], s));
+    }
+#pragma unroll
+    for (int k = 1; k < LANES; k *= 2) s += __shfl_xor(s, k);  // (all lanes of a row are in the loop together)
+    m = s <= FLT_MAX ? fmaxf(m, s) : m;
+  }
+#pragma unroll
+  for (int k = LANES; k < 64; k *= 2) m = fmaxf(m, __shfl_xor(m, k));
+  if ((threadIdx.x & 63) == 0) most[threadIdx.x >> 6] = m;
+  __syncthreads();
+  if (threadIdx.x == 0) p.sizes[blockIdx.x] = fmaxf(fmaxf(most[0], most[1]), fmaxf(most[2], most[3]));
+}
+
+// The largest of a key head's pieces, the same in every lane.
+__device__ __forceinline__ void largest_squares(const WindowDims &p, int b, int hk, float &of_do, float &of_v) {
+  const int lane = threadIdx.x & 63;
+  const float *const at = p.sizes + ((size_t)b * p.Hkv + hk) * (p.do_slots + p.v_slots);
+  float d = 0.f, v = 0.f;
+  for (int i = lane; i < p.do_slots; i += 64) d = fmaxf(d, at[i]);
+  for (int i = lane; i < p.v_slots; i += 64) v = fmaxf(v, at[p.do_slots + i]);
+#pragma unroll
+  for (int k = 1; k < 64; k *= 2) {
+    d = fmaxf(d, __shfl_xor(d, k));
+    v = fmaxf(v, __shfl_xor(v, k));
+  }
+  of_do = __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, d)));
+  of_v = __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, v)));
+}
+
 // ---- dQ -----------------------------------------------------------------------------------------------------
 // 128 queries to a workgroup, two workgroups per CU: eight waves of one workgroup on the same tiles read them half as often,
 // but wait for each other (655 us two, 700 one, also with a barrier for every second tile and three tiles on their way).
@@ -209,11 +310,14 @@ __global__ __launch_bounds__(256, 2) void window_attn_dq_kernel(
   const int i0 = r * BQ, i1 = min(i0 + BQ, e.q_len), col = i0 + w.wave * Tile::COLS + w.l32;
   const size_t row0 = (size_t)bh * p.Nq;
   f32x16 dq[DB];
+  float ds_unit = 1.f;  // what dQ's sums are to be multiplied by: 1 / F
 #pragma unroll
   for (int db = 0; db < DB; ++db)
 #pragma unroll
     for (int v = 0; v < 16; ++v) dq[db][v] = 0.f;
   if (i0 < i1) {
+    float most_do = 0.f, most_v = 0.f;
+    if constexpr (GradScale<T>::FOLLOWS) largest_squares(p, b, h / (p.Hq / p.Hkv), most_do, most_v);
     const Tiles tiles(p, e, i0, i1);
     // tiles [t0, t0 + n) of the block, counted from 0 below
     const int t0 = (int)((long long)tiles.n * part / p.dq_parts), n_tiles = (int)((long long)tiles.n * (part + 1) / p.dq_parts) - t0;
@@ -239,8 +343,9 @@ __global__ __launch_bounds__(256, 2) void window_attn_dq_kernel(
     const float lse2 = sees ? z * 1.4426950408889634f - GradScale<T>::P_LOG2 : INFINITY;
 #pragma unroll
     for (int s = 0; s < DS; ++s) dout[s] = sees ? dout[s] : u32x4{0, 0, 0, 0};
-    float dl = 0.f;
+    float dl = 0.f, ds_of_p = 1.f;  // ds_of_p: factor of dP - delta beside P as kept
     {
+      float square = 0.f;
       u32x4 o[DS];
       w.operand(gout + (size_t)b * p.out.b + (size_t)h * p.out.h + (size_t)row * p.out.n, o);
 #pragma unroll
@@ -253,12 +358,20 @@ __global__ __launch_bounds__(256, 2) void window_attn_dq_kernel(
           T::unpack(y, y2);
           dl = __builtin_fmaf(x2[0], y2[0], dl);
           dl = __builtin_fmaf(x2[1], y2[1], dl);
+          if constexpr (GradScale<T>::FOLLOWS) square = __builtin_fmaf(x2[0], x2[0], __builtin_fmaf(x2[1], x2[1], square));
         }
       dl = sum_with_other_half(dl);
-      dl *= Tile::DS_OF_P;
+      float dl_keys = dl;
+      if constexpr (GradScale<T>::FOLLOWS) {
+        const float f = grad_factor(sum_with_other_half(square), most_v);
+        ds_unit = 1.f / f;
+        ds_of_p = f * GradScale<T>::P_UNIT;
+        dl_keys = dl * (grad_factor(most_do, most_v) * GradScale<T>::P_UNIT);
+        dl *= ds_of_p;
+      }
       if (w.g == 0 && col < i1 && part == 0) {  // for dK and dV: [head][lse2, delta][query]
         stats[2 * row0 + col] = lse2;
-        stats[2 * row0 + p.Nq + col] = dl;
+        stats[2 * row0 + p.Nq + col] = dl_keys;
       }
     }
     // dO in AGPRs, beside dQ: the compiler halves the registers, and the VGPRs are for the rest
@@ -321,7 +434,7 @@ __global__ __launch_bounds__(256, 2) void window_attn_dq_kernel(
             s[v + 1] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[v + 1], sc, -lse2));
           }
           if constexpr (Tile::dq_ds_gap(u) == g)
-            ds[v >> 3][(v >> 1) & 3] = T::pack(s[v] * __builtin_fmaf(dp[v], Tile::DS_OF_P, -dl), s[v + 1] * __builtin_fmaf(dp[v + 1], Tile::DS_OF_P, -dl));
+            ds[v >> 3][(v >> 1) & 3] = T::pack(s[v] * ds_factor(dp[v], ds_of_p, dl), s[v + 1] * ds_factor(dp[v + 1], ds_of_p, dl));
         });
         __builtin_amdgcn_sched_barrier(0);
       });
@@ -346,38 +459,14 @@ __global__ __launch_bounds__(256, 2) void window_attn_dq_kernel(
     for (int db = 0; db < DB; ++db)
 #pragma unroll
       for (int a = 0; a < 4; ++a)
-        *reinterpret_cast<f32x4 *>(to + 32 * db + 8 * a) = f32x4{dq[db][4 * a], dq[db][4 * a + 1], dq[db][4 * a + 2], dq[db][4 * a + 3]};
+        *reinterpret_cast<f32x4 *>(to + 32 * db + 8 * a) =
+            f32x4{dq[db][4 * a] * ds_unit, dq[db][4 * a + 1] * ds_unit, dq[db][4 * a + 2] * ds_unit, dq[db][4 * a + 3] * ds_unit};
   } else {
-    Tile::store(dq, p.scale / GradScale<T>::DS, col < i1, gdq + (size_t)b * p.dq.b + (size_t)h * p.dq.h + (size_t)col * p.dq.n, w.g);
+    Tile::store(dq, p.scale * ds_unit, col < i1, gdq + (size_t)b * p.dq.b + (size_t)h * p.dq.h + (size_t)col * p.dq.n, w.g);
   }
 }
 
 // ---- dK, dV -------------------------------------------------------------------------------------------------
-// The queries that see keys [j0, j1) (j1 within k_len): of the window between two positions, of the sinks all from the
-// first on.
-struct WindowQueries {
-  int begin, end;
-  static __device__ __forceinline__ int floor_div(int x, int y) {
-    const int f = x / y;
-    return f - (f * y > x);
-  }
-  // first query that sees key j, last + 1 that does
-  static __device__ __forceinline__ int first_of(const WindowDims &p, const WindowEntry &e, int j) {
-    if (p.right < 0) return 0;
-    const long long pos = ((long long)j / p.frame - p.right) * p.frame - e.start;
-    return (int)min(max(pos, 0ll), (long long)e.q_len);
-  }
-  static __device__ __forceinline__ int end_of(const WindowDims &p, const WindowEntry &e, int j) {
-    if (p.left < 0 || j < p.sinks) return e.q_len;
-    const long long pos = ((long long)j / p.frame + p.left + 1) * p.frame - e.start;
-    return (int)min(max(pos, 0ll), (long long)e.q_len);
-  }
-  __device__ __forceinline__ WindowQueries(const WindowDims &p, const WindowEntry &e, int j0, int j1) {
-    begin = first_of(p, e, j0);
-    end = j0 < p.sinks ? e.q_len : end_of(p, e, j1 - 1);
-  }
-};
-
 // Units of work of one key head: the blocks that hold sinks in bwd_sink_parts parts each, the others in bwd_parts.
 __device__ __forceinline__ int grad_units(const WindowDims &p, int n_blocks) {
   return p.n_sink_blocks * p.bwd_sink_parts + (n_blocks - p.n_sink_blocks) * p.bwd_parts;
@@ -434,11 +523,20 @@ __global__ __launch_bounds__(512, 2) void window_attn_dkv_kernel(
   for (int db = 0; db < DB; ++db)
 #pragma unroll
     for (int v = 0; v < 16; ++v) dk[db][v] = dv[db][v] = 0.f;
+  float ds_unit = 1.f;  // what dK's sums are to be multiplied by: 1 / F
   if (j0 < j1) {
     const WindowQueries seen(p, e, j0, j1);
     const int n_tiles = max(0, seen.end - seen.begin + ROWS - 1) / ROWS;
     const int u0 = (int)((long long)G * n_tiles * part / parts), u1 = (int)((long long)G * n_tiles * (part + 1) / parts);
     if (u0 < u1) {
+      float ds_of_p = 1.f;
+      if constexpr (GradScale<T>::FOLLOWS) {
+        float most_do, most_v;
+        largest_squares(p, b, hk, most_do, most_v);
+        const float f = grad_factor(most_do, most_v);
+        ds_unit = 1.f / f;
+        ds_of_p = f * GradScale<T>::P_UNIT;
+      }
       const uint32_t q_bytes = (uint32_t)p.q.n * 2, do_bytes = (uint32_t)p.dout.n * 2;
       const uint32_t q_limit = (uint32_t)(seen.end - 1) * q_bytes + Tile::ROWB, do_limit = (uint32_t)(seen.end - 1) * do_bytes + Tile::ROWB;
       // the tile that is asked for next: its head's rows, and the first of them
@@ -570,7 +668,7 @@ __global__ __launch_bounds__(512, 2) void window_attn_dkv_kernel(
             }
             if constexpr (PH + Tile::ds_gap(u_) == g) {
               const f32x2 dl = row_stat[(8 + u_) % RING];
-              ds[n >> 3][(n >> 1) & 3] = T::pack(s[n] * __builtin_fmaf(dp[n], Tile::DS_OF_P, -dl[0]), s[n + 1] * __builtin_fmaf(dp[n + 1], Tile::DS_OF_P, -dl[1]));
+              ds[n >> 3][(n >> 1) & 3] = T::pack(s[n] * ds_factor(dp[n], ds_of_p, dl[0]), s[n + 1] * ds_factor(dp[n + 1], ds_of_p, dl[1]));
             }
           });
           __builtin_amdgcn_sched_barrier(0);
@@ -598,15 +696,16 @@ __global__ __launch_bounds__(512, 2) void window_attn_dkv_kernel(
     for (int db = 0; db < DB; ++db)
 #pragma unroll
       for (int a = 0; a < 4; ++a) {
-        *reinterpret_cast<f32x4 *>(to_k + 32 * db + 8 * a) = f32x4{dk[db][4 * a], dk[db][4 * a + 1], dk[db][4 * a + 2], dk[db][4 * a + 3]};
+        *reinterpret_cast<f32x4 *>(to_k + 32 * db + 8 * a) =
+            f32x4{dk[db][4 * a] * ds_unit, dk[db][4 * a + 1] * ds_unit, dk[db][4 * a + 2] * ds_unit, dk[db][4 * a + 3] * ds_unit};
         *reinterpret_cast<f32x4 *>(to_v + 32 * db + 8 * a) = f32x4{dv[db][4 * a], dv[db][4 * a + 1], dv[db][4 * a + 2], dv[db][4 * a + 3]};
       }
     return;
   }
   const bool there = col < j1;  // rows behind the keys: zeros, their columns repeat the last key
   const size_t at = (size_t)b * p.dkv.b + (size_t)hk * p.dkv.h + (size_t)col * p.dkv.n;
-  Tile::store(dk, p.scale / GradScale<T>::DS, there, gdk + at, w.g);
-  Tile::store(dv, Tile::P_UNIT, there, gdv + at, w.g);
+  Tile::store(dk, p.scale * ds_unit, there, gdk + at, w.g);
+  Tile::store(dv, GradScale<T>::P_UNIT, there, gdv + at, w.g);
 }
 
 // Sums of the parts of every key's row, and behind them of every query's, in the order of the parts, rounded once.
@@ -624,7 +723,7 @@ __global__ __launch_bounds__(256) void window_attn_grad_sum_kernel(uint16_t *__r
   size_t step;
   int parts, b;
   uint16_t *to;
-  float f = p.scale / GradScale<T>::DS;
+  float f = p.scale;
   bool there;
   if (item < of_keys) {
     const int which = (int)(item & 1), key = (int)((item >> 1) % cut), bh = (int)((item >> 1) / cut), hk = bh % p.Hkv;
@@ -637,7 +736,7 @@ __global__ __launch_bounds__(256) void window_attn_grad_sum_kernel(uint16_t *__r
     parts = sink ? p.bwd_sink_parts : p.bwd_parts;
     b = bh / p.Hkv;
     to = (which ? gdv : gdk) + (size_t)b * p.dkv.b + (size_t)hk * p.dkv.h + (size_t)key * p.dkv.n;
-    if (which) f = Tile::P_UNIT;
+    if (which) f = GradScale<T>::P_UNIT;
     there = key < (p.k_len ? min(p.k_len[b], p.Nk) : p.Nk);
   } else {
     const long long row = item - of_keys, n = (long long)p.B * p.Hq * p.Nq;

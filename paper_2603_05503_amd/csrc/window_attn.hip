@@ -141,7 +141,9 @@ int launch_forward(ForwardForm form, const uint16_t *q, const uint16_t *k, const
 // gets parts as long as the others'.
 struct GradPlan {
   int dq_parts, parts, sink_parts, sink_blocks;
-  int64_t bytes;  // of the workspace: lse and delta of every query, and the sums of the parts
+  int do_slots, v_slots;  // pieces whose largest rows of dO and V are found apart (fp16)
+  int64_t sums_bytes;     // of lse and delta of every query, and the sums of the parts
+  int64_t bytes;          // of the workspace: those, and the sizes of the pieces
 };
 GradPlan grad_plan(int B, int Hq, int Hkv, int Nq, int Nk, int D, const calibatt_window &w) {
   GradPlan g;
@@ -173,10 +175,13 @@ GradPlan grad_plan(int B, int Hq, int Hkv, int Nq, int Nk, int D, const calibatt
   // keys so far: 107 us whole, 82 in four parts; 8 heads of 875, three frames of 134, D = 64: 51 and, in two, 45)
   const int64_t q_rows = (int64_t)B * Hq * Nq, q_units = (int64_t)B * Hq * ((Nq + 127) / 128);
   g.dq_parts = (int)std::max<int64_t>(1, std::min<int64_t>({2 * WINDOW_CUS / q_units, window_tiles(w, 128, Nk, ROWS) / 8, WINDOW_MAX_PARTS}));
-  g.bytes = (q_rows + 1) / 2 * 16 + (g.dq_parts > 1 ? g.dq_parts * q_rows * D * 4 : 0);
+  g.sums_bytes = (q_rows + 1) / 2 * 16 + (g.dq_parts > 1 ? g.dq_parts * q_rows * D * 4 : 0);
   const int64_t row = 2 * D * 4;
-  if (g.parts > 1) g.bytes += g.parts * heads * Nk * row;
-  if (g.sink_blocks && g.sink_parts > 1) g.bytes += g.sink_parts * heads * g.sink_blocks * BLOCK * row;
+  if (g.parts > 1) g.sums_bytes += g.parts * heads * Nk * row;
+  if (g.sink_blocks && g.sink_parts > 1) g.sums_bytes += g.sink_parts * heads * g.sink_blocks * BLOCK * row;
+  g.do_slots = (int)std::min<int64_t>(SIZE_MAX_SLOTS, (G * Nq + SIZE_ROWS - 1) / SIZE_ROWS);
+  g.v_slots = (int)std::min<int64_t>(SIZE_MAX_SLOTS, (Nk + SIZE_ROWS - 1) / SIZE_ROWS);
+  g.bytes = g.sums_bytes + heads * (g.do_slots + g.v_slots) * 4;
   return g;
 }
 
@@ -200,6 +205,11 @@ int launch_backward(const GradTensors &t, const WindowDims &p, hipStream_t strea
   const int64_t sums = 2 * cut * p.B * p.Hkv + (p.dq_parts > 1 ? (int64_t)p.B * p.Hq * p.Nq : 0);
   const int64_t per_wg = 256 / (D / 8), sum_wgs = (sums + per_wg - 1) / per_wg;
   if (q_units > MAX_GRID || k_units > MAX_GRID || sum_wgs > MAX_GRID) return CALIBATT_ERR_SHAPE;
+  if constexpr (GradScale<T>::FOLLOWS) {
+    const int64_t pieces = (int64_t)p.B * p.Hkv * (p.do_slots + p.v_slots);
+    if (pieces > MAX_GRID) return CALIBATT_ERR_SHAPE;
+    if (int st = launch_kernel(window_attn_sizes_kernel<D>, (unsigned)pieces, 256, 0, stream, t.dout, t.v, p)) return st;
+  }
   if (int st = launch_kernel(window_attn_dq_kernel<D, T>, (unsigned)(8 * ((q_units + 7) / 8)), 256, DQ_LDS, stream, t.dout, t.q, t.k,
                              t.v, t.out, t.lse, t.dq, t.stats, p))
     return st;
@@ -287,6 +297,9 @@ extern "C" int calibatt_window_attn_bwd(const void *dout, const void *q, const v
   p.n_sink_blocks = g.sink_blocks;
   p.part_dq = (float *)workspace + ((int64_t)B * Hq * Nq + 1) / 2 * 4;
   p.part_dkv = p.part_dq + (g.dq_parts > 1 ? (int64_t)g.dq_parts * B * Hq * Nq * D : 0);
+  p.sizes = (float *)((char *)workspace + g.sums_bytes);
+  p.do_slots = g.do_slots;
+  p.v_slots = g.v_slots;
   const GradTensors t = {(const uint16_t *)dout, (const uint16_t *)q, (const uint16_t *)k, (const uint16_t *)v,
                          (const uint16_t *)out, lse, (uint16_t *)dq, (uint16_t *)dk, (uint16_t *)dv, (float *)workspace};
   hipStream_t s = (hipStream_t)stream;

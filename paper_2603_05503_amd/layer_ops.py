@@ -442,7 +442,8 @@ def window_attn_fwd(q, k, v, out, window: Window, scale: float, lse=None, q_star
 def window_attn_bwd(dout, q, k, v, out, lse, window: Window, scale: float, dq=None, dk=None, dv=None, q_start=None, q_len=None,
                     k_len=None, stream=None):
     """calibatt_window_attn_bwd: (dq, dk, dv) for ``dout``, the gradient of what ``window_attn_fwd`` left in ``out`` for the same
-    arguments, and its ``lse``; new tensors unless given (dk and dv share their strides, no result may be an input)."""
+    arguments, and its ``lse``; new tensors unless given (dk and dv share their strides, no result may be an input).  fp16: dout
+    may be of any size, that of a scaled loss among them, as long as the gradients themselves are within the type."""
     import torch
 
     lib = _b.load_library()
