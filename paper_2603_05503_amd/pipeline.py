@@ -45,19 +45,29 @@ class QKPreparation:
 
     def __call__(self, q, k, geometry=None, stream=None):
         """(q, k) prepared, on the call's stream: new tensors, or with ``in_place`` the given ones."""
-        fresh = not self.in_place
+        return self._prepare(q, k, geometry, stream, *((q, k) if self.in_place else (None, None)))
+
+    def packed(self, q, k, geometry=None):
+        """(q, k) prepared on the current stream, as packed [B, H, N, D] tensors whatever the given ones' layout; those stay as
+        they are, also with ``in_place``."""
+        import torch
+
+        to = (torch.empty(t.shape, dtype=t.dtype, device=t.device) for t in (q, k))
+        q, k = self._prepare(q, k, geometry, None, *to)
+        return q.contiguous(), k.contiguous()  # (one that nothing is done to comes as it was given)
+
+    def _prepare(self, q, k, geometry, stream, q_to, k_to):
+        """``q_to``, ``k_to``: tensors that receive the prepared ones, None: new ones."""
+        grid = geometry if self.grid is None else self.grid
+        if self.rope is not None and grid is None:
+            raise ValueError("a rotation needs a grid, or a caller with a geometry")
+        # what the norm made is turned where it is
         if self.q_norm is not None:
-            q = _l.layer_norm_fwd(q, *self.q_norm, eps=self.eps, center=self.center, out=None if fresh else q, stream=stream)
+            q = q_to = _l.layer_norm_fwd(q, *self.q_norm, eps=self.eps, center=self.center, out=q_to, stream=stream)
         if self.k_norm is not None:
-            k = _l.layer_norm_fwd(k, *self.k_norm, eps=self.eps, center=self.center, out=None if fresh else k, stream=stream)
+            k = k_to = _l.layer_norm_fwd(k, *self.k_norm, eps=self.eps, center=self.center, out=k_to, stream=stream)
         if self.rope is not None:
-            grid = geometry if self.grid is None else self.grid
-            if grid is None:
-                raise ValueError("a rotation needs a grid, or a caller with a geometry")
-            # what the norm made is turned where it is
-            q, k = _l.rope_axes(q, k, self.rope, grid=grid, start=self.start, stream=stream,
-                                q_out=None if fresh and self.q_norm is None else q,
-                                k_out=None if fresh and self.k_norm is None else k)
+            q, k = _l.rope_axes(q, k, self.rope, grid=grid, start=self.start, stream=stream, q_out=q_to, k_out=k_to)
         return q, k
 
 
@@ -77,11 +87,12 @@ class Calibrator:
     def observe(self, key: Hashable, q, k, eps: float, scale: float) -> None:
         """One dense forward's q, k ([B, H, N, D] bf16 CUDA tensors; every batch element counts as a
         prompt) at the step/layer ``key``, with the energy threshold ``eps`` of that step.  With ``prepare`` they come as the
-        projections leave them, and are normalised and turned first."""
+        projections leave them, in any layout that it takes, and are normalised and turned first, in tensors of this call's
+        own: the given ones stay as they are, also with an ``in_place`` preparation.  Without, they are packed."""
         import torch
 
         if self.prepare is not None:
-            q, k = self.prepare(q, k, self.geometry)
+            q, k = self.prepare.packed(q, k, self.geometry)
         # energy -> Eq. 6 -> one more vote per block, all on the device; the counters come back in finalize
         if self._energy_workspace is None or self._energy_workspace.device != q.device:
             nbytes = _b.block_energy_workspace_bytes(self.N, self.block_q, self.block_k)
