@@ -85,7 +85,7 @@ bool window_strides(const calibatt_strides *given, int B, int H, int N, int D, b
   if (B == 1) s.b = 0;
   if (H == 1) s.h = 0;
   if (N == 1) s.n = D;
-  if (s.n < D || s.b < 0 || s.h < 0 || s.n % 8 || s.h % 8 || s.b % 8) return false;
+  if (s.n < D || s.n > 0x7fffffff || s.b < 0 || s.h < 0 || s.n % 8 || s.h % 8 || s.b % 8) return false;
   // The kernels address the rows of one head with 32-bit byte offsets, also those behind the last one that a tile or a block
   // of 256 still has: they have to lie behind a descriptor's end, and not past 2^32 at the head's first rows again.
   return ((unsigned long long)N + 256) * (unsigned long long)s.n * 2 <= 0xffffffffULL;
