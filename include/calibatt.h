@@ -752,6 +752,9 @@ typedef struct calibatt_rope_place {
  * calibatt_sparse_attn_fwd_strided (NULL = packed; every one a multiple of 8, n
  * >= D, pointers 16-byte aligned; no limit on a head's bytes).  An output may be
  * its own input with the same strides and must not overlap an input otherwise.
+ * The rows of an output must lie apart, here and in the calls below (SHAPE; also
+ * for layouts that are neither nested nor small enough to look through, more than
+ * 2^16 differences of indices along the two shorter axes).
  * Arithmetic is fp32, rounded once.
  * Errors: NULL; SHAPE (also: more channels than D, a grid of more than N tokens
  * or beyond the tables, B or a number of heads above 65535); UNSUPPORTED (dtype,

@@ -31,10 +31,11 @@ int device_cus(int &cus) {
 }
 
 // ---- rotary positions ---------------------------------------------------------------------------------------
-// Strides of a tensor; those of an axis of one entry are never stepped along.  No two rows of an output may start in one.
+// Strides of a tensor; those of an axis of one entry are never stepped along.  No two rows of an output may overlap.
 bool rope_strides(const calibatt_strides *given, int B, int H, int N, int D, bool output, Strides &s) {
   s = given ? Strides{given->b, given->h, given->n} : Strides{(int64_t)H * N * D, (int64_t)N * D, D};
-  if (output && ((B > 1 && s.b < D) || (H > 1 && s.h < D))) return false;
+  const int64_t sizes[3] = {B, H, N}, steps[3] = {s.b, s.h, s.n};
+  if (output && !rows_apart(sizes, steps, D)) return false;
   if (B == 1) s.b = 0;
   if (H == 1) s.h = 0;
   if (N == 1) s.n = D;
@@ -149,11 +150,12 @@ int norm_check(int64_t B, int64_t H, int64_t N, int C, int dtype, int weight_dty
     return CALIBATT_ERR_UNSUPPORTED;
   return CALIBATT_OK;
 }
-// `row`: elements that lie between two rows at least: C for an output, 0 for an input, whose rows may be one
+// `row`: C for an output, whose rows must not overlap, 0 for an input, whose rows may be one
 bool norm_tensor_ok(const void *ptr, const int64_t n[3], const calibatt_strides &s, int bytes, int row) {
   const int64_t step[3] = {s.b, s.h, s.n};
   for (int i = 0; i < 3; ++i)
-    if (step[i] < 0 || (n[i] > 1 && step[i] < row)) return false;
+    if (step[i] < 0) return false;
+  if (row && !rows_apart(n, step, row)) return false;
   return ((uintptr_t)ptr & (bytes - 1)) == 0;
 }
 

@@ -78,10 +78,11 @@ int window_check(int B, int Hq, int Hkv, int Nq, int Nk, int D, const calibatt_w
   return CALIBATT_OK;
 }
 
-// Strides of a tensor; those of an axis of one entry are never stepped along.  No two rows of an output may start in one.
+// Strides of a tensor; those of an axis of one entry are never stepped along.  No two rows of an output may overlap.
 bool window_strides(const calibatt_strides *given, int B, int H, int N, int D, bool output, Strides &s) {
   s = given ? Strides{given->b, given->h, given->n} : Strides{(int64_t)H * N * D, (int64_t)N * D, D};
-  if (output && ((B > 1 && s.b < D) || (H > 1 && s.h < D))) return false;
+  const int64_t sizes[3] = {B, H, N}, steps[3] = {s.b, s.h, s.n};
+  if (output && !rows_apart(sizes, steps, D)) return false;
   if (B == 1) s.b = 0;
   if (H == 1) s.h = 0;
   if (N == 1) s.n = D;
