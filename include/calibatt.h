@@ -843,6 +843,17 @@ typedef struct calibatt_window {
 int calibatt_window_attn_workspace_bytes(int B, int Hq, int Hkv, int Nq, int Nk, int D,
                                          const calibatt_window *window, int64_t *forward,
                                          int64_t *backward);
+/* How a call of these sizes is run (host, no GPU needed): the kernel of its
+ * forward, and the pieces that the keys of a block of queries are cut into (with
+ * a workspace), and, of the gradients, those of a block of queries (dq_parts)
+ * and of the queries of a block of 256 keys (dkv_parts; sink_parts for the first
+ * sink_blocks of them, which hold sinks).  Errors: as the workspace's. */
+enum { CALIBATT_WINDOW_BLOCKS_128 = 0, CALIBATT_WINDOW_BLOCKS_32 = 1, CALIBATT_WINDOW_SHARED_ROWS = 2 };
+typedef struct calibatt_window_form {
+  int32_t forward, forward_parts, dq_parts, dkv_parts, sink_parts, sink_blocks;
+} calibatt_window_form;
+int calibatt_window_attn_form(int B, int Hq, int Hkv, int Nq, int Nk, int D, const calibatt_window *window,
+                              calibatt_window_form *form);
 int calibatt_window_attn_fwd(const void *q, const void *k, const void *v, void *out, float *lse, int B,
                              int Hq, int Hkv, int Nq, int Nk, int D, const calibatt_window *window,
                              float scale, const calibatt_strides *q_strides,

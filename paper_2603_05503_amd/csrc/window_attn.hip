@@ -29,7 +29,7 @@ int64_t window_tiles(const calibatt_window &w, int n, int Nk, int tile) {
 }
 
 // Which kernel a forward goes through.
-enum ForwardForm { BLOCKS_128, BLOCKS_32, SHARED_ROWS };
+enum ForwardForm { BLOCKS_128 = CALIBATT_WINDOW_BLOCKS_128, BLOCKS_32 = CALIBATT_WINDOW_BLOCKS_32, SHARED_ROWS = CALIBATT_WINDOW_SHARED_ROWS };
 // Workgroups of the kernel for few queries that the GPU holds (its LDS, 128 KB at D = 128).
 int64_t step_slots(int D) { return D == 128 ? WINDOW_CUS : 2 * WINDOW_CUS; }
 ForwardForm forward_form(int B, int Hq, int Hkv, int Nq, int Nk, int D, const calibatt_window &w) {
@@ -229,6 +229,17 @@ extern "C" int calibatt_window_attn_workspace_bytes(int B, int Hq, int Hkv, int 
   const ForwardForm form = forward_form(B, Hq, Hkv, Nq, Nk, D, *window);
   *forward = forward_bytes(forward_parts(form, B, Hq, Hkv, Nq, Nk, D, *window), B, Hq, Nq, D);
   *backward = grad_plan(B, Hq, Hkv, Nq, Nk, D, *window).bytes;
+  return CALIBATT_OK;
+}
+
+extern "C" int calibatt_window_attn_form(int B, int Hq, int Hkv, int Nq, int Nk, int D, const calibatt_window *window,
+                                         calibatt_window_form *form) {
+  if (!window || !form) return CALIBATT_ERR_NULL;
+  if (int st = window_check(B, Hq, Hkv, Nq, Nk, D, *window)) return st;
+  const ForwardForm forward = forward_form(B, Hq, Hkv, Nq, Nk, D, *window);
+  const GradPlan g = grad_plan(B, Hq, Hkv, Nq, Nk, D, *window);
+  *form = calibatt_window_form{forward, forward_parts(forward, B, Hq, Hkv, Nq, Nk, D, *window), g.dq_parts, g.parts, g.sink_parts,
+                               g.sink_blocks};
   return CALIBATT_OK;
 }
 

@@ -39,6 +39,8 @@ def declare(lib):
         C.c_float, C.c_int, C.c_int, C.c_int, C.c_void_p, C.c_int64, C.c_void_p]
     lib.calibatt_window_attn_workspace_bytes.restype = C.c_int
     lib.calibatt_window_attn_workspace_bytes.argtypes = [C.c_int] * 6 + [C.c_void_p, i64p, i64p]
+    lib.calibatt_window_attn_form.restype = C.c_int
+    lib.calibatt_window_attn_form.argtypes = [C.c_int] * 6 + [C.c_void_p] * 2
     lib.calibatt_window_attn_fwd.restype = C.c_int
     lib.calibatt_window_attn_fwd.argtypes = [C.c_void_p] * 5 + [C.c_int] * 6 + [C.c_void_p, C.c_float] + [C.c_void_p] * 3 + [
         C.c_int, C.c_void_p, C.c_int64, C.c_void_p]
@@ -326,6 +328,14 @@ class _CWindow(C.Structure):
                 ("q_start", C.c_void_p), ("q_len", C.c_void_p), ("k_len", C.c_void_p)]
 
 
+class _CWindowForm(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("forward", "forward_parts", "dq_parts", "dkv_parts", "sink_parts", "sink_blocks")]
+
+
+# forms of a window's forward, see Window.form
+WINDOW_BLOCKS_128, WINDOW_BLOCKS_32, WINDOW_SHARED_ROWS = 0, 1, 2
+
+
 class Window:
     """Which keys a query sees (``calibatt_window``): those of ``left`` frames before its own to ``right`` frames behind it
     (-1: all), and the first ``sinks`` keys that are not ahead of that.  ``frame``: tokens of a frame (1: a window of
@@ -367,6 +377,14 @@ class Window:
                 self._bytes.clear()
             n = self._bytes[key] = fwd.value, bwd.value
         return n
+
+    def form(self, B: int, Hq: int, Hkv: int, Nq: int, Nk: int, D: int):
+        """calibatt_window_attn_form: how a call of these sizes is run, as a dict (``forward``: WINDOW_*)."""
+        c, f = _CWindow(*self._values), _CWindowForm()
+        st = _b.load_library().calibatt_window_attn_form(B, Hq, Hkv, Nq, Nk, D, C.addressof(c), C.addressof(f))
+        if st != 0:
+            raise _b.CalibattError(st, "calibatt_window_attn_form")
+        return {name: getattr(f, name) for name, _ in f._fields_}
 
 
 def _window_plan(key, window, q, k, v, others, kv_like=()):
