@@ -76,8 +76,9 @@ constexpr __host__ __device__ int il_iv_cols(int bq) { return bq == 64 ? 1024 : 
 
 // The base class lays out LDS and lanes for a window of two sub-tiles of K and of V.  EXACT_SUM: a row's sum is that of the
 // probabilities in fp32 and not of what they are rounded to for the second contraction (one more instruction per pair): a
-// log-sum-exp then has the precision that a gradient computed from it needs.
-template <int D, int BQ, int BK, typename T = Bf16, bool EXACT_SUM = false>
+// log-sum-exp then has the precision that a gradient computed from it needs.  P_LOG2: probabilities, and with them the row sum,
+// are kept times 2^P_LOG2 (the reference that they are relative to is that much lower than m_run).
+template <int D, int BQ, int BK, typename T = Bf16, bool EXACT_SUM = false, int P_LOG2 = 0>
 struct IlRow : RowBlock<D, BQ, 2 * il_sub(D, BQ, BK), T> {
   using RB = RowBlock<D, BQ, 2 * il_sub(D, BQ, BK), T>;
   using RB::DB;
@@ -190,14 +191,14 @@ struct IlRow : RowBlock<D, BQ, 2 * il_sub(D, BQ, BK), T> {
       psum[0] = 0.f;
       psum[1] = 0.f;
       // a little less than IL_REF_SLACK: the product is not rounded here as it is below
-      moved = __any(__builtin_fmaf(part[0], sc, neg_ref) > IL_REF_SLACK - 0.01f);
+      moved = __any(__builtin_fmaf(part[0], sc, neg_ref) > IL_REF_SLACK - 0.01f + P_LOG2);
       if (moved) {
         const float rm = max_with_other_half(part[0]) * sc;
         const float m_old = this->m_run;
         const float m_new = rm - m_old > IL_REF_SLACK ? rm : m_old;  // rm > m_old where it is taken
         alpha = __builtin_amdgcn_exp2f(m_old - m_new);  // 0 on the first sub-tile; 1 where nothing moves
         this->m_run = m_new;
-        neg_ref = -m_new;
+        neg_ref = P_LOG2 - m_new;
       }
     } else {
       constexpr int g = (J - OPS_MAX - 1) / OPS_GROUP, o = (J - OPS_MAX - 1) % OPS_GROUP;

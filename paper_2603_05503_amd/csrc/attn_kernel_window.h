@@ -103,12 +103,17 @@ __device__ __forceinline__ void window_head(int x, int B, int G, int &b, int &h)
   h = hk * G + (x - group * G);
 }
 
+// fp16 has few exponents, and long rows many small probabilities: they are kept times 2^15 (shared rows, blocks of 32) and 2^7 of
+// what they are relative to the running reference, which the interleaved engine leaves up to 2^8 below a row's largest.
+template <typename T> constexpr int BLOCKS_P_LOG2 = std::is_same<T, F16>::value ? 7 : 0;
+template <typename T> constexpr int STEP_P_LOG2 = std::is_same<T, F16>::value ? 15 : 0;
+
 // ---- blocks of 128 queries ----------------------------------------------------------------------------------
 // The interleaved engine (attn_kernel_il.h) over the tiles of a block: its stages, its softmax beside the MFMAs, its
 // two workgroups per CU.  What differs is where the tiles are, and that the mask is an interval per query.
 template <int D, typename T>
-struct WindowRow : IlRow<D, 128, 64, T, true> {
-  using Base = IlRow<D, 128, 64, T, true>;
+struct WindowRow : IlRow<D, 128, 64, T, true, BLOCKS_P_LOG2<T>> {
+  using Base = IlRow<D, 128, 64, T, true, BLOCKS_P_LOG2<T>>;
   using Base::EL;
   using Base::V_S;
   using Base::Base;
@@ -244,6 +249,7 @@ __global__ __launch_bounds__(256, 2) __attribute__((amdgpu_num_vgpr(IL_VGPRS))) 
     wait_vmem<0>();
   }
   __syncthreads();  // every wave is done with the tile windows
+  rb.m_run -= BLOCKS_P_LOG2<T>;  // what the sums are relative to
   const size_t row0 = ((size_t)bh * p.Nq) + i0;
   if (p.parts > 1) {
     if (i >= p.Nq) return;
@@ -384,11 +390,12 @@ __global__ __launch_bounds__(STEP_WAVES * 64) void window_attn_step_kernel(
       const float m_new = fmaxf(m_run, max_with_other_half(m_loc));  // finite: leading keys at -inf have no weight
       const float alpha = __builtin_amdgcn_exp2f(m_run - m_new);
       m_run = m_new;
+      const float ref = m_new - STEP_P_LOG2<T>;
       l_run *= alpha;
       uint32_t pk[8];
 #pragma unroll
       for (int v = 0; v < 16; v += 2) {
-        const float p0 = __builtin_amdgcn_exp2f(s[v] - m_new), p1 = __builtin_amdgcn_exp2f(s[v + 1] - m_new);
+        const float p0 = __builtin_amdgcn_exp2f(s[v] - ref), p1 = __builtin_amdgcn_exp2f(s[v + 1] - ref);
         l_run += p0 + p1;
         pk[v >> 1] = T::pack(p0, p1);
       }
@@ -415,6 +422,7 @@ __global__ __launch_bounds__(STEP_WAVES * 64) void window_attn_step_kernel(
     asm volatile("s_waitcnt vmcnt(0)" : : : "memory");  // nothing is written to LDS behind this
   }
   l_run = sum_with_other_half(l_run);
+  m_run -= STEP_P_LOG2<T>;  // what the sums are relative to
   __syncthreads();
   // join the waves' sums: rows [wave][32][JOIN_STRIDE], then their references and row sums
   float *const rows = reinterpret_cast<float *>(lds), *const ml = rows + STEP_WAVES * 32 * Lds::JOIN_STRIDE;
