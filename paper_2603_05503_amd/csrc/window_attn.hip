@@ -39,8 +39,9 @@ ForwardForm forward_form(int B, int Hq, int Hkv, int Nq, int Nk, int D, const ca
   // whose four waves take a fourth of the keys each, have four times as many chains of half the length, but read every key
   // four times as often.  They are faster where they all run at once, for up to about 48 tiles each.  Us, D = 64 / 128, all
   // keys so far, blocks of 128 (in parts) and of 32: 2 heads of 128 queries on 1024 keys 16 and 12 / 18 and 16; 8 heads of
-  // 1024 17 and 12 / 22 and 17; 8 of 1024 on 4096 27.5 and 27.8 / 33 and 54; 16 of 1024 19 and 15 / 26 and 22 (two rounds:
-  // not taken), on 3000 30 and 34 / 40 and 64.
+  // 1024 17 and 12 / 22 and 17; 8 of 1024 on 4096 27.5 and 27.8 / 33 and 54; 16 of 1024 19 and 15 / 26 and 22, on 3000 30 and
+  // 34 / 40 and 64.  (At D = 128 the 512 blocks of 16 heads are two rounds, which the rule leaves to blocks of 128: 4 us more
+  // on 1024 keys, 24 less on 3000.)
   const int64_t units = (int64_t)B * Hq * ((Nq + 31) / 32);
   if (units <= step_slots(D) && units * window_tiles(w, 32, Nk, STEP_KEYS) <= 48 * step_slots(D)) return BLOCKS_32;
   return BLOCKS_128;
