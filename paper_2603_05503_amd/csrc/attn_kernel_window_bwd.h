@@ -224,18 +224,18 @@ __global__ __launch_bounds__(256) void window_attn_sizes_kernel(const uint16_t *
   const int slots = p.do_slots + p.v_slots, bh = blockIdx.x / slots, slot = blockIdx.x - bh * slots, b = bh / p.Hkv, hk = bh - b * p.Hkv;
   const int G = p.Hq / p.Hkv, c = 8 * (threadIdx.x % LANES);
   const bool of_do = slot < p.do_slots;
-  // G Nq and Nk rows, each within 31 bits
+  // G Nq and Nk rows, each within 31 bits, but not what is stepped beyond them
   const int rows = of_do ? G * p.Nq : p.Nk, piece = of_do ? slot : slot - p.do_slots, pieces = of_do ? p.do_slots : p.v_slots;
   const int first = (int)((long long)rows * piece / pieces), last = (int)((long long)rows * (piece + 1) / pieces);
   const WindowEntry e(p, b);
   float m = 0.f;
   const uint16_t *const do_group = gdo + (size_t)b * p.dout.b + (size_t)hk * G * p.dout.h, *const v_head = gv + (size_t)b * p.kv.b + (size_t)hk * p.kv.h;
-  for (int r0 = first + threadIdx.x / LANES; r0 < last; r0 += FLIGHT * ROWS) {
+  for (long long r0 = (long long)first + threadIdx.x / LANES; r0 < last; r0 += FLIGHT * ROWS) {
     u32x4 raw[FLIGHT];
     bool seen[FLIGHT];
 #pragma unroll
     for (int n = 0; n < FLIGHT; ++n) {
-      const int r = min(r0 + n * ROWS, last - 1);
+      const int r = (int)min(r0 + n * ROWS, (long long)last - 1);
       const uint16_t *row;
       if (of_do) {
         const int g = r / p.Nq, i = r - g * p.Nq;
