@@ -825,7 +825,8 @@ typedef struct calibatt_window {
  * all bf16 or all fp16; Hq a multiple of Hkv, query head h reads key head
  * h / (Hq / Hkv).  out = softmax(scale q K^T) V over the visible keys, fp32
  * accumulation, probabilities rounded to the element type for the product with
- * V; a query that sees no key gets zeros.  lse (NULL, or DEVICE fp32 packed
+ * V (fp16: times 2^7 at least of what they are of a row's largest, so that small
+ * ones stay within its range); a query that sees no key gets zeros.  lse (NULL, or DEVICE fp32 packed
  * [B][Hq][Nq]): the natural logarithm of the sum of exponentials, -inf there.
  * Keys and values that no query of a call's block sees are not read; those that
  * some query sees must be finite.
